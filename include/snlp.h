@@ -30,6 +30,7 @@
 #ifndef SNLP_H_
 #define SNLP_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -285,6 +286,83 @@ int snlp_graph_count(const snlp_model *m, int64_t *captured);
 #define SNLP_STATIC_LM_HEAD_MAX_D_MODEL 4096
 int snlp_lm_head_greedy_static(const float *hL, const void *lm_head_bf16, int rows, int n_streams, int d_model, int vocab,
                                float rms_eps, int32_t *argmax, void *stream);
+
+/* ---- key/value cache held in 4 bits, in pages -------------------------------------------------------------------
+ * Operators of a cache that holds keys and values in 4 bits and requests of different lengths; they need no model
+ * handle (snlp_kv_create_4bit is the cache of a model that runs on them).  They use the current CUDA device, which must
+ * be the one their pointers belong to, and only enqueue work on `stream`; they allocate nothing, keep nothing between
+ * calls and may be captured into CUDA graphs.  The paper has no counterpart: a K-sweep decode step reads the cache K
+ * times, which is why a smaller cache pays here.
+ *
+ * Format.  The head_dim features (64 or 128) of one token of one head are cut into groups of 64.  A group is 64 codes
+ * c in 0..15 and a bf16 pair (s, m): value = s * c + m.  With lo, hi the group's smallest and largest element,
+ *   s = bf16(fp32((hi - lo) / 15)),  m = bf16(lo),  c = round-half-even((x - m) / s) limited to 0..15  (c = 0 where s = 0);
+ * a group with a NaN or an infinity in it, or whose s or m is beyond bf16's range, is stored with s = m = NaN.
+ * The pool is [n_pages][n_kv_head][page_size / 16] blocks of 16 tokens; a block is
+ *   key codes [16][head_dim/2] | key (s, m) [16][head_dim/64][2] | value codes | value (s, m),
+ * i.e. 16 * 2 * (head_dim/2 + head_dim/16) bytes.  Features 8j .. 8j+7 share a little-endian 32-bit word, feature i of it in
+ * bits 4(i%8) .. ; with g = j / 8, r = j % 8 and G = head_dim / 64 the word's place in its row is
+ * (r/2)*2G + 2g + r%2 for keys and r*G + g for values.
+ * A token's slot is page * page_size + offset; block_table[b][i] is the page of positions i*page_size .. of sequence b. */
+typedef struct {
+  void *pages;                                  /* device, 16-byte aligned, snlp_kv4_pool_bytes bytes             */
+  int32_t n_pages, page_size;                   /* page_size: a power of two in 16..1024                          */
+  int32_t n_kv_head, head_dim;                  /* head_dim: 64 or 128                                            */
+} snlp_kv4_pool;
+/* Size of a pool (its `pages` pointer is not looked at).  Errors: ARG, UNSUPPORTED. */
+int snlp_kv4_pool_bytes(const snlp_kv4_pool *pool, size_t *bytes);
+
+/* Block tables and slot maps from request lengths, on the device.  Sequence b holds ctx_lens[b] tokens and gets new_lens[b]
+ * (>= 0) more.  The pages it lacks, ceil((ctx+new)/page_size) - ceil(ctx/page_size), are taken in sequence order from
+ * free_pages[*free_head ..] and entered into its row of block_table [B][max_pages]; entries below ceil(ctx/page_size) are
+ * only read, the others left as they are.  free_pages == NULL: no page is taken, the table already has them all.
+ *   slots     [max_tokens] int64: of the new tokens, sequence after sequence; -1 from the last token on
+ *   positions [max_tokens] (nullable): their positions; -1 likewise        cu_new [B+1] (nullable): prefix sums of new_lens
+ *   lens      [B]: ctx + new (not one of the inputs)                       info [2] (nullable): pages taken, status
+ * status 0: served.  Otherwise nothing is taken or entered, every slot and position is -1, cu_new is 0 and lens = ctx (0 where
+ * negative); bits: 1 too few free pages, 2 a row needs more than max_pages pages, 4 more than max_tokens new tokens,
+ * 8 a negative length or a position beyond int32.  All pointers are device memory; free_head (nullable = 0) is read, not
+ * advanced: the caller adds info[0].  A negative table entry gives slot -1.
+ * Errors: ARG (NULL, misaligned, page_size, sizes), SHAPE (B > 4096, max_tokens > 2^30), CUDA. */
+int snlp_page_plan(const int32_t *ctx_lens, const int32_t *new_lens, int B, int page_size, const int32_t *free_pages, int n_free,
+                   const int32_t *free_head, int32_t *block_table, int max_pages, int max_tokens, int64_t *slots,
+                   int32_t *positions, int32_t *cu_new, int32_t *lens, int32_t *info, void *stream);
+
+/* Store keys and values k, v [n][n_kv_head][head_dim] (device; dtype SNLP_DTYPE_*) at slots [n] (device int64).  Tokens whose
+ * slot lies outside the pool are left out.  The slots of one call must differ: of two tokens with one slot the row may hold
+ * parts of both.  strides (host int64[4], nullable = dense): token and head stride of k, token and head stride of v, in
+ * elements; the head_dim features of a row are contiguous.
+ * Errors: ARG (NULL, misaligned, dtype, page_size, negative n or stride), UNSUPPORTED (head_dim), SHAPE, CUDA. */
+int snlp_kv4_write(const snlp_kv4_pool *pool, const void *k, const void *v, int dtype, const int64_t *strides, const int64_t *slots, int n,
+                   void *stream);
+/* The rows at slots [n] as k, v (rounded to dtype; strides as in snlp_kv4_write); zeros where a slot lies outside the pool. */
+int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const int64_t *strides, const int64_t *slots, int n, void *stream);
+
+/* Causal attention over the pages.  Sequence b has lens[b] keys (its new rows' among them: write first, then attend) and
+ * T_b query rows, the last T_b of its positions: row i sees keys 0 .. lens[b] - T_b + i.  Query head h reads key/value head
+ * h / (n_head / n_kv_head).  A row that sees no key is zero.  Keys on a page outside 0..n_pages-1 count as value 0 and
+ * score 0 (an error of the caller's that reads nothing out of bounds).
+ *   cu_q  device int32 [B+1], nullable: rows cu_q[b] .. cu_q[b+1]-1 of q and out are sequence b's (ascending; rows behind
+ *         cu_q[B] are left as they are); NULL: n_rows / B rows each
+ *   max_len  no length is above it (longer ones are cut); 0 = max_pages * page_size.  It sizes the workspace.
+ *   scale  of the scores; 0 = 1/sqrt(head_dim)
+ * out [n_rows][n_head][head_dim], q's dtype, dense.  bf16 results: probabilities are rounded to 11 bits before the second
+ * product; fp32 results: queries and probabilities are split in two such terms (22 bits); all sums are fp32.
+ * A row's result depends on its own query, its visible keys and B * n_kv_head only, bit for bit.
+ * workspace (device, 16-byte aligned, snlp_kv4_attention_workspace bytes, may be NULL if that is 0) needs no initial
+ * contents; calls that may overlap on the GPU need one each.
+ * Errors: ARG, SHAPE (B > 4096, too many rows), UNSUPPORTED (head_dim), CUDA. */
+typedef struct {
+  const void *q;                        /* device [n_rows][n_head][head_dim]                             */
+  int64_t q_token_stride, q_head_stride; /* elements (>= 0); dense: n_head * head_dim, head_dim          */
+  const int32_t *block_table;           /* device [B][max_pages]                                         */
+  const int32_t *lens;                  /* device [B]                                                    */
+  const int32_t *cu_q;                  /* device [B+1], nullable                                        */
+  int32_t dtype, n_rows, B, n_head, max_pages, max_len;
+  float scale;
+} snlp_kv4_attn;
+int snlp_kv4_attention_workspace(const snlp_kv4_pool *pool, const snlp_kv4_attn *args, size_t *bytes);
+int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn *args, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 const char *snlp_last_error(void);
 

@@ -1,0 +1,291 @@
+// Key/value cache held in 4 bits: launchers and C entry points (snlp_page_plan, snlp_kv4_*).
+#include "../../include/snlp.h"
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <mutex>
+
+#include "kv4.cuh"
+
+namespace snlp {
+void set_last_error(const char *msg);  // defined next to snlp_last_error()
+
+// ------------------------------------------------------------------------------------------------
+// launchers
+cudaError_t kv4_plan(const Kv4Plan &p, cudaStream_t st) {
+  const int blocks = std::max(1, (int)(((int64_t)p.max_tokens + kPlanTokens - 1) / kPlanTokens));
+  k_kv4_plan<<<blocks, kPlanThreads, 2 * (size_t)(p.B + 1) * sizeof(int), st>>>(p);
+  return cudaGetLastError();
+}
+
+// 16-byte accesses need every row to start on such a boundary
+static bool rows_vec(const Kv4Rows &p) {
+  const size_t u = p.fp32 ? 4 : 8;   // elements in 16 bytes
+  auto ok = [&](const void *x, size_t ls, size_t ts, size_t hs) { return (uintptr_t)x % 16 == 0 && ls % u == 0 && ts % u == 0 && hs % u == 0; };
+  return ok(p.k, p.k_ls, p.k_ts, p.k_hs) && ok(p.v, p.v_ls, p.v_ts, p.v_hs);
+}
+
+template <bool WRITE>
+static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
+  if (p.n < 1) return cudaSuccess;
+  const dim3 grid((unsigned)((p.n + kKv4Block - 1) / kKv4Block) * p.H, p.nl);
+  const bool vec = rows_vec(p);
+#define KV4_ROWS(T, HD)                                                       \
+  do {                                                                        \
+    if (WRITE) k_kv4_write<T, HD><<<grid, kRowsThreads(HD), 0, st>>>(p, vec); \
+    else k_kv4_read<T, HD><<<grid, kRowsThreads(HD), 0, st>>>(p, vec);        \
+  } while (0)
+  if (p.fp32) {
+    if (p.hd == 128) KV4_ROWS(float, 128); else KV4_ROWS(float, 64);
+  } else {
+    if (p.hd == 128) KV4_ROWS(__nv_bfloat16, 128); else KV4_ROWS(__nv_bfloat16, 64);
+  }
+#undef KV4_ROWS
+  return cudaGetLastError();
+}
+cudaError_t kv4_write(const Kv4Rows &p, cudaStream_t st) { return rows_launch<true>(p, st); }
+cudaError_t kv4_read(const Kv4Rows &p, cudaStream_t st) { return rows_launch<false>(p, st); }
+
+// Keys of a split.  It depends on the number of (sequence, key/value head) pairs only, as in the attention over the
+// unquantised cache: not on lengths, query rows or layers, so that every call merges a row's keys in the same order.
+int kv4_chunk(int pairs) { return pairs < 32 ? 256 : pairs < 256 ? 512 : 1024; }
+
+static int chunks_max(int B, int Hkv, int max_len) {
+  const int c = kv4_chunk(B * Hkv);
+  return (int)(((int64_t)max_len + c - 1) / c);
+}
+
+size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl) {
+  const int n = chunks_max(B, Hkv, max_len);
+  return n < 2 ? 0 : (size_t)nl * n_rows * Hq * n * (hd + 4) * sizeof(float);
+}
+
+template <typename T, int HD, int NT>
+static cudaError_t attn_attr() {
+  return cudaFuncSetAttribute(k_kv4_attn<T, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn4Smem<HD, NT>::kFixed + (kKv4MaxBatch + 1) * 4);
+}
+template <typename T, int HD>
+static cudaError_t attn_attr2() {
+  const cudaError_t e = attn_attr<T, HD, 1>();
+  return e != cudaSuccess ? e : attn_attr<T, HD, 2>();
+}
+
+cudaError_t kv4_init() {
+  static std::mutex mu;
+  static bool done[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mu);
+  if (dev < 64 && done[dev]) return cudaSuccess;
+  e = attn_attr2<float, 64>();
+  if (e == cudaSuccess) e = attn_attr2<float, 128>();
+  if (e == cudaSuccess) e = attn_attr2<__nv_bfloat16, 64>();
+  if (e == cudaSuccess) e = attn_attr2<__nv_bfloat16, 128>();
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv4_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (kKv4MaxBatch + 1) * 4);
+  if (e == cudaSuccess && dev < 64) done[dev] = true;
+  return e;
+}
+
+template <typename T, int HD, int NT>
+static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) {
+  const Kv4Attn &a = p.a;
+  typedef Attn4Smem<HD, NT> S;
+  const size_t smem = S::kFixed + (size_t)(a.B + 1) * 4;
+  const int resident = std::min<int>(NT == 1 ? 3 : 2, (int)((size_t)228 * 1024 / (smem + 1024 + 64)));   // 64: the kernel's static arrays
+  // at most this many units; the kernel counts the real ones from the lengths on the device
+  const int64_t most = ((int64_t)a.n_rows * p.G / (8 * NT) + a.B) * p.nch_max * a.Hkv * a.nl;
+  const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)n_sm * resident));
+  k_kv4_attn<T, HD, NT><<<grid, kAttn4Threads, smem, st>>>(p);
+  if (p.nch_max > 1) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.n_rows * a.Hq, a.nl); cfg.blockDim = dim3(128); cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // scheduled while the splits finish, waits for their results
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, k_kv4_merge<T, HD>, p, 8 * NT);
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
+  Attn4Params p{};
+  p.a = a;
+  p.G = a.Hq / a.Hkv;
+  p.chunk = kv4_chunk(a.B * a.Hkv);
+  p.nch_max = std::max(1, chunks_max(a.B, a.Hkv, a.max_len));
+  p.qk_scale = a.scale * 1.4426950408889634f;
+  const size_t u = a.fp32 ? 4 : 8;
+  p.vec = (uintptr_t)a.q % 16 == 0 && a.q_ls % u == 0 && a.q_ts % u == 0 && a.q_hs % u == 0;
+  // one tile of 8 query rows a unit where a sequence brings no more (decoding), two beyond: the codes are unpacked once for
+  // 16 rows instead of 8
+  const bool two = (int64_t)a.n_rows * p.G > (int64_t)8 * a.B;
+#define KV4_ATTN(T, HD) (two ? attn_launch<T, HD, 2>(p, n_sm, st) : attn_launch<T, HD, 1>(p, n_sm, st))
+  if (a.fp32) return a.hd == 128 ? KV4_ATTN(float, 128) : KV4_ATTN(float, 64);
+  return a.hd == 128 ? KV4_ATTN(__nv_bfloat16, 128) : KV4_ATTN(__nv_bfloat16, 64);
+#undef KV4_ATTN
+}
+
+}  // namespace snlp
+
+// ------------------------------------------------------------------------------------------------
+// C entry points
+using namespace snlp;
+
+static int refuse(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  set_last_error(buf);
+  return code;
+}
+
+static int launched(cudaError_t e, const char *who) {
+  return e == cudaSuccess ? SNLP_OK : refuse(SNLP_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+}
+
+static int check_page(int page, const char *who) {
+  if (page < kKv4Block || page > 1024 || (page & (page - 1))) return refuse(SNLP_ERR_ARG, "%s: page_size must be a power of two in 16..1024 (got %d)", who, page);
+  return SNLP_OK;
+}
+
+static int check_pool(const snlp_kv4_pool *pool, const char *who) {
+  if (!pool || !pool->pages) return refuse(SNLP_ERR_ARG, "%s: NULL pool", who);
+  if ((uintptr_t)pool->pages % 16) return refuse(SNLP_ERR_ARG, "%s: the pool must be 16-byte aligned", who);
+  if (pool->n_pages < 1 || pool->n_kv_head < 1) return refuse(SNLP_ERR_ARG, "%s: n_pages and n_kv_head must be >= 1", who);
+  if (pool->head_dim != 64 && pool->head_dim != 128) return refuse(SNLP_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %d)", who, pool->head_dim);
+  return check_page(pool->page_size, who);
+}
+
+extern "C" int snlp_kv4_pool_bytes(const snlp_kv4_pool *pool, size_t *bytes) {
+  const char *who = "snlp_kv4_pool_bytes";
+  if (!pool || !bytes) return refuse(SNLP_ERR_ARG, "%s: NULL argument", who);
+  snlp_kv4_pool p = *pool;
+  p.pages = (void *)16;   // not looked at
+  const int rc = check_pool(&p, who);
+  if (rc != SNLP_OK) return rc;
+  *bytes = (size_t)p.n_pages * p.n_kv_head * (p.page_size / kKv4Block) * kv4_block_bytes(p.head_dim);
+  return SNLP_OK;
+}
+
+extern "C" int snlp_page_plan(const int32_t *ctx_lens, const int32_t *new_lens, int B, int page_size, const int32_t *free_pages, int n_free,
+                              const int32_t *free_head, int32_t *block_table, int max_pages, int max_tokens, int64_t *slots,
+                              int32_t *positions, int32_t *cu_new, int32_t *lens, int32_t *info, void *stream) {
+  const char *who = "snlp_page_plan";
+  if (!ctx_lens || !new_lens || !block_table || !lens || (!slots && max_tokens > 0)) return refuse(SNLP_ERR_ARG, "%s: NULL pointer", who);
+  if ((uintptr_t)ctx_lens % 4 || (uintptr_t)new_lens % 4 || (uintptr_t)free_pages % 4 || (uintptr_t)free_head % 4 || (uintptr_t)block_table % 4 ||
+      (uintptr_t)positions % 4 || (uintptr_t)cu_new % 4 || (uintptr_t)lens % 4 || (uintptr_t)info % 4 || (uintptr_t)slots % 8)
+    return refuse(SNLP_ERR_ARG, "%s: int32 pointers must be 4-byte aligned, slots 8-byte aligned", who);
+  if (B < 1 || max_pages < 1 || max_tokens < 0 || n_free < 0) return refuse(SNLP_ERR_ARG, "%s: B and max_pages must be >= 1, max_tokens and n_free >= 0", who);
+  if (B > kKv4MaxBatch) return refuse(SNLP_ERR_SHAPE, "%s: B = %d exceeds %d", who, B, kKv4MaxBatch);
+  if (max_tokens > (1 << 30)) return refuse(SNLP_ERR_SHAPE, "%s: max_tokens = %d exceeds %d", who, max_tokens, 1 << 30);
+  if (lens == ctx_lens || lens == new_lens) return refuse(SNLP_ERR_ARG, "%s: lens must not be one of the inputs", who);
+  int rc = check_page(page_size, who);
+  if (rc != SNLP_OK) return rc;
+  if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
+  Kv4Plan p{};
+  p.ctx = ctx_lens; p.ctx_stride = 1; p.add = new_lens; p.B = B; p.page = page_size;
+  p.free_pages = free_pages; p.n_free = n_free; p.free_head = free_head;
+  p.table = block_table; p.tstride = max_pages; p.max_tokens = max_tokens;
+  p.slots = slots; p.positions = positions; p.cu = cu_new; p.lens = lens; p.info = info;
+  return launched(kv4_plan(p, (cudaStream_t)stream), who);
+}
+
+static int rows_call(bool write, const snlp_kv4_pool *pool, void *k, void *v, int dtype, const int64_t *strides, const int64_t *slots, int n,
+                     void *stream, const char *who) {
+  int rc = check_pool(pool, who);
+  if (rc != SNLP_OK) return rc;
+  if (n < 0) return refuse(SNLP_ERR_ARG, "%s: n must be >= 0", who);
+  if (dtype != SNLP_DTYPE_FP32 && dtype != SNLP_DTYPE_BF16) return refuse(SNLP_ERR_ARG, "%s: unknown dtype %d", who, dtype);
+  if (n == 0) return SNLP_OK;
+  if (!k || !v || !slots) return refuse(SNLP_ERR_ARG, "%s: NULL pointer", who);
+  const size_t es = dtype == SNLP_DTYPE_FP32 ? 4 : 2;
+  if ((uintptr_t)k % es || (uintptr_t)v % es || (uintptr_t)slots % 8) return refuse(SNLP_ERR_ARG, "%s: k and v must be aligned to their element, slots to 8 bytes", who);
+  Kv4Rows p{};
+  p.k = k; p.v = v; p.nl = 1;
+  const int64_t dense[4] = {(int64_t)pool->n_kv_head * pool->head_dim, pool->head_dim, (int64_t)pool->n_kv_head * pool->head_dim, pool->head_dim};
+  const int64_t *s = strides ? strides : dense;
+  for (int i = 0; i < 4; ++i)
+    if (s[i] < 0) return refuse(SNLP_ERR_ARG, "%s: strides must be >= 0", who);
+  p.k_ts = s[0]; p.k_hs = s[1]; p.v_ts = s[2]; p.v_hs = s[3];
+  p.pool = (uint8_t *)pool->pages; p.slots = slots; p.n = n; p.H = pool->n_kv_head; p.hd = pool->head_dim; p.page = pool->page_size;
+  p.n_slots = (int64_t)pool->n_pages * pool->page_size;
+  p.fp32 = dtype == SNLP_DTYPE_FP32;
+  if ((int64_t)((n + (int64_t)kKv4Block - 1) / kKv4Block) * p.H > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
+  return launched(write ? kv4_write(p, (cudaStream_t)stream) : kv4_read(p, (cudaStream_t)stream), who);
+}
+
+extern "C" int snlp_kv4_write(const snlp_kv4_pool *pool, const void *k, const void *v, int dtype, const int64_t *strides, const int64_t *slots, int n,
+                              void *stream) {
+  return rows_call(true, pool, const_cast<void *>(k), const_cast<void *>(v), dtype, strides, slots, n, stream, "snlp_kv4_write");
+}
+
+extern "C" int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const int64_t *strides, const int64_t *slots, int n, void *stream) {
+  return rows_call(false, pool, k, v, dtype, strides, slots, n, stream, "snlp_kv4_read");
+}
+
+static int attn_check(const snlp_kv4_attn *a, const snlp_kv4_pool *pool, const char *who) {
+  if (!a || !pool) return refuse(SNLP_ERR_ARG, "%s: NULL argument", who);
+  if (a->dtype != SNLP_DTYPE_FP32 && a->dtype != SNLP_DTYPE_BF16) return refuse(SNLP_ERR_ARG, "%s: unknown dtype %d", who, a->dtype);
+  if (a->B < 1 || a->n_rows < 0 || a->n_head < 1 || a->max_pages < 1) return refuse(SNLP_ERR_ARG, "%s: B, n_head and max_pages must be >= 1, n_rows >= 0", who);
+  if (a->B > kKv4MaxBatch) return refuse(SNLP_ERR_SHAPE, "%s: B = %d exceeds %d", who, a->B, kKv4MaxBatch);
+  if (a->n_head % pool->n_kv_head) return refuse(SNLP_ERR_ARG, "%s: n_head = %d is not a multiple of n_kv_head = %d", who, a->n_head, pool->n_kv_head);
+  if (!a->cu_q && a->n_rows % a->B) return refuse(SNLP_ERR_ARG, "%s: without cu_q every sequence has n_rows / B rows: %d is not a multiple of %d", who, a->n_rows, a->B);
+  if (a->max_len < 0) return refuse(SNLP_ERR_ARG, "%s: max_len must be >= 0", who);
+  const int64_t cap = (int64_t)a->max_pages * pool->page_size;
+  if (cap > 0x7fffffffLL - 2048) return refuse(SNLP_ERR_SHAPE, "%s: max_pages * page_size exceeds the positions of a sequence", who);
+  return SNLP_OK;
+}
+
+static int attn_max_len(const snlp_kv4_attn *a, const snlp_kv4_pool *pool) {
+  const int cap = a->max_pages * pool->page_size;
+  return a->max_len > 0 && a->max_len < cap ? a->max_len : cap;
+}
+
+extern "C" int snlp_kv4_attention_workspace(const snlp_kv4_pool *pool, const snlp_kv4_attn *args, size_t *bytes) {
+  const char *who = "snlp_kv4_attention_workspace";
+  if (!bytes || !pool) return refuse(SNLP_ERR_ARG, "%s: NULL argument", who);
+  snlp_kv4_pool p = *pool;
+  p.pages = (void *)16;   // not looked at
+  int rc = check_pool(&p, who);
+  if (rc != SNLP_OK || (rc = attn_check(args, pool, who)) != SNLP_OK) return rc;
+  *bytes = kv4_workspace(args->n_rows, args->B, args->n_head, pool->n_kv_head, pool->head_dim, attn_max_len(args, pool), 1);
+  return SNLP_OK;
+}
+
+extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn *args, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  const char *who = "snlp_kv4_attention";
+  int rc = check_pool(pool, who);
+  if (rc != SNLP_OK || (rc = attn_check(args, pool, who)) != SNLP_OK) return rc;
+  if (args->n_rows == 0) return SNLP_OK;
+  if (!args->q || !args->block_table || !args->lens || !out) return refuse(SNLP_ERR_ARG, "%s: NULL pointer", who);
+  const size_t es = args->dtype == SNLP_DTYPE_FP32 ? 4 : 2;
+  if ((uintptr_t)args->q % es || (uintptr_t)out % es || (uintptr_t)args->block_table % 4 || (uintptr_t)args->lens % 4 || (uintptr_t)args->cu_q % 4)
+    return refuse(SNLP_ERR_ARG, "%s: q and out must be aligned to their element, int32 arrays to 4 bytes", who);
+  if (args->q_token_stride < 0 || args->q_head_stride < 0) return refuse(SNLP_ERR_ARG, "%s: strides must be >= 0", who);
+  if (!(args->scale == args->scale)) return refuse(SNLP_ERR_ARG, "%s: scale is not a number", who);
+  Kv4Attn a{};
+  a.max_len = attn_max_len(args, pool);
+  const size_t need = kv4_workspace(args->n_rows, args->B, args->n_head, pool->n_kv_head, pool->head_dim, a.max_len, 1);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return refuse(SNLP_ERR_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : (size_t)0, need);
+  if ((uintptr_t)workspace % 16) return refuse(SNLP_ERR_ARG, "%s: the workspace must be 16-byte aligned", who);
+  const int64_t G = args->n_head / pool->n_kv_head;
+  const int64_t units = (args->n_rows * G / 8 + args->B) * (int64_t)(((int64_t)a.max_len + 255) / 256);
+  if (units > 0x7fffffffLL || (int64_t)args->n_rows * args->n_head > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
+  if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
+  int dev = 0, n_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+  if ((rc = launched(e, who)) != SNLP_OK) return rc;
+  a.q = args->q; a.q_ts = args->q_token_stride; a.q_hs = args->q_head_stride;
+  a.pool = (const uint8_t *)pool->pages; a.table = args->block_table; a.tstride = args->max_pages; a.lens = args->lens; a.cu = args->cu_q;
+  a.out = out; a.part = (float *)workspace;
+  a.T = args->n_rows / args->B; a.n_rows = args->n_rows; a.B = args->B; a.Hq = args->n_head; a.Hkv = pool->n_kv_head; a.hd = pool->head_dim;
+  a.n_pages = pool->n_pages; a.page = pool->page_size; a.nl = 1; a.fp32 = args->dtype == SNLP_DTYPE_FP32;
+  a.scale = args->scale != 0.f ? args->scale : (pool->head_dim == 128 ? 0.08838834764831845f : 0.125f);
+  return launched(kv4_attention(a, n_sm, (cudaStream_t)stream), who);
+}

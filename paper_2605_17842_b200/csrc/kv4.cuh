@@ -1,0 +1,1037 @@
+// Kernels of the key/value cache held in 4 bits: page plan, write, read, attention.
+//
+// Format.  A row (the hd features of one token of one head) is cut into groups of 64; a group is stored as 64 codes of
+// 4 bits and a bf16 pair (s, m): value = s * c + m.  A block of 16 tokens of one head is contiguous -- key codes | key
+// parameters | value codes | value parameters -- and a page holds, per head, page/16 blocks, so the 16 keys of one matrix
+// instruction and their values are one run of 2304 bytes (hd 128).  Feature f of a word sits in bits 4 (f % 8); the words
+// of a row are ordered for the reader: a thread of the attention kernel finds all it needs of a row in one 16-byte
+// (keys) or 8-byte (values) load, without bank conflicts.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "kv4.h"
+
+namespace snlp {
+
+template <int HD>
+struct Kv4Fmt {
+  static constexpr int NG = HD / kKv4Group;
+  static constexpr int kCodes = HD / 2, kPar = 4 * NG;           // bytes of a row
+  static constexpr int KC = 0, KP = kKv4Block * kCodes, VC = KP + kKv4Block * kPar, VP = VC + kKv4Block * kCodes;
+  static constexpr int kBytes = 2 * VC;
+  static_assert(kBytes == kv4_block_bytes(HD), "block size");
+  // word of features 8j .. 8j+7 within a row
+  __device__ static int key_word(int j) { return ((j & 7) >> 1) * (2 * NG) + 2 * (j >> 3) + (j & 1); }
+  __device__ static int val_word(int j) { return (j & 7) * NG + (j >> 3); }
+};
+
+// ---------------------------------------------------------------------------------------------------
+// Plan.  With h_b = ceil(ctx_b / P) pages held and e_b = ceil((ctx_b + new_b) / P) needed, sequence b takes free pages
+// off_b .. off_b + e_b - h_b - 1 (off = exclusive prefix sum), and token i of the flattened new tokens belongs to the
+// sequence with cu_b <= i < cu_{b+1}, at position ctx_b + i - cu_b.  Every block repeats the two prefix sums over the
+// lengths (a few kilobytes, from L2) and then serves its own share of tokens and new pages by binary search: one launch, no
+// block waits for another.  Bound by latency: launch, one read of the lengths, the scan, one dependent table read.
+// A call that cannot be served (status below) takes no page, leaves the table alone and marks every slot -1.
+constexpr int kPlanThreads = 256;
+constexpr int kPlanTokens = 1024;   // tokens per block
+enum { KV4_PLAN_PAGES = 1, KV4_PLAN_TABLE = 2, KV4_PLAN_TOKENS = 4, KV4_PLAN_LENGTH = 8 };
+
+// block-wide exclusive scan of two 64-bit values per thread; returns the totals through t0, t1
+__device__ __forceinline__ void plan_scan(long long &a, long long &b, long long &t0, long long &t1, long long (*red)[2]) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long a0 = a, b0 = b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
+    if (lane >= o) { a += x; b += y; }
+  }
+  if (lane == 31) { red[w][0] = a; red[w][1] = b; }
+  __syncthreads();
+  long long pa = 0, pb = 0;
+  t0 = t1 = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / 32; ++i) {
+    const long long x = red[i][0], y = red[i][1];
+    if (i < w) { pa += x; pb += y; }
+    t0 += x; t1 += y;
+  }
+  a += pa - a0;
+  b += pb - b0;
+  __syncthreads();
+}
+
+// largest b in [0, n) with off[b] <= i (off ascending, off[0] <= i)
+__device__ __forceinline__ int find_seq(const int *off, int n, int i) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= i) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+static __global__ void __launch_bounds__(kPlanThreads) k_kv4_plan(Kv4Plan p) {
+  extern __shared__ int plan_sm[];
+  int *s_cu = plan_sm, *s_off = plan_sm + p.B + 1;   // exclusive prefix sums: new tokens, new pages
+  __shared__ long long red[kPlanThreads / 32][2];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  long long tok = 0, pages = 0;
+  for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    long long n = 0, np = 0;
+    if (b < p.B) {
+      const long long c = p.ctx[(size_t)b * p.ctx_stride], a = p.add ? p.add[b] : p.add_const;
+      const long long have = (c + p.page - 1) / p.page, need = (c + a + p.page - 1) / p.page;
+      if (c < 0 || a < 0 || c + a > 0x7fffffffLL) atomicOr(&s_bad, KV4_PLAN_LENGTH);
+      else {
+        if (need > p.tstride) atomicOr(&s_bad, KV4_PLAN_TABLE);
+        n = a;
+        np = p.free_pages ? need - have : 0;
+      }
+    }
+    long long t0, t1;
+    plan_scan(n, np, t0, t1, red);
+    // sums beyond 32 bits are refused below (max_tokens and n_free are ints): the truncated entries are not used then
+    if (b < p.B) { s_cu[b] = (int)(tok + n); s_off[b] = (int)(pages + np); }
+    tok += t0;
+    pages += t1;
+  }
+  const int head = p.free_head ? max(*p.free_head, 0) : 0;
+  if (tid == 0) {
+    s_cu[p.B] = (int)tok;
+    s_off[p.B] = (int)pages;
+    if (tok > p.max_tokens) s_bad |= KV4_PLAN_TOKENS;
+    if (pages > 0 && pages > (long long)p.n_free - head) s_bad |= KV4_PLAN_PAGES;
+  }
+  __syncthreads();
+  const int bad = s_bad, ntok = bad ? 0 : (int)tok, npages = bad ? 0 : (int)pages;
+  if (blockIdx.x == 0) {
+    for (int b = tid; b <= p.B; b += kPlanThreads) {
+      if (p.cu) p.cu[b] = bad ? 0 : s_cu[b];
+      if (b < p.B) {
+        const int c = max(p.ctx[(size_t)b * p.ctx_stride], 0);
+        p.lens[b] = bad ? c : c + (p.add ? p.add[b] : p.add_const);
+      }
+    }
+    if (tid == 0 && p.info) { p.info[0] = npages; p.info[1] = bad; }
+  }
+  // new pages into the table, dealt over all blocks
+  for (int i = blockIdx.x * kPlanThreads + tid; i < npages; i += gridDim.x * kPlanThreads) {
+    const int b = find_seq(s_off, p.B, i), c = p.ctx[(size_t)b * p.ctx_stride];
+    p.table[(size_t)b * p.tstride + (int)(((long long)c + p.page - 1) / p.page) + i - s_off[b]] = p.free_pages[head + i];
+  }
+  const int first = blockIdx.x * kPlanTokens;
+  for (int i = first + tid; i < min(first + kPlanTokens, p.max_tokens); i += kPlanThreads) {
+    long long slot = -1;
+    int pos = -1;
+    if (i < ntok) {
+      const int b = find_seq(s_cu, p.B, i), c = p.ctx[(size_t)b * p.ctx_stride];
+      pos = c + i - s_cu[b];
+      const int j = pos / p.page, have = (int)(((long long)c + p.page - 1) / p.page);
+      // a page taken by this call is read from the free list: another block may not have entered it yet
+      const int pg = (p.free_pages && j >= have) ? p.free_pages[head + s_off[b] + j - have] : p.table[(size_t)b * p.tstride + j];
+      slot = pg < 0 ? -1 : (long long)pg * p.page + pos % p.page;
+    }
+    p.slots[i] = slot;
+    if (p.positions) p.positions[i] = pos;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Write.  Per (token, head, group): lo = min x, hi = max x; s = bf16(fp32((hi - lo) / 15)), m = bf16(lo);
+// c = round-half-even((x - m) / s) in 0..15 (0 where s = 0).  A group that holds a NaN or an infinity, or whose s or m leaves
+// bf16's range, is stored with s = m = NaN: what reads it sees NaN instead of a silently wrong number.
+// A thread holds 8 features (one word of codes) of a key row and of the same value row; 8 threads share a group.  A block
+// covers 16 consecutive tokens of one head, so the rows of a storage block are written together.  Bound by HBM: each input
+// is read once and each code written once.
+__device__ __forceinline__ float min_nan(float a, float b) {   // NaN if either is (fminf would drop it)
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// rounding error of the difference d = fl(a - b): a - b = d + err exactly
+__device__ __forceinline__ float diff_err(float a, float b, float d) {
+  const float bb = __fsub_rn(d, a);
+  return __fsub_rn(__fsub_rn(a, __fsub_rn(d, bb)), __fadd_rn(b, bb));
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, bool vec, float (&x)[8]);
+template <>
+__device__ __forceinline__ void load8<float>(const float *p, bool vec, float (&x)[8]) {
+  if (vec) {
+    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
+  }
+}
+template <>
+__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, bool vec, float (&x)[8]) {
+  if (vec) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+  }
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, bool vec, const float (&x)[8]);
+template <>
+__device__ __forceinline__ void store8<float>(float *p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = x[i];
+  }
+}
+template <>
+__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+  }
+}
+
+// Codes of 8 features of a group whose 64 lie in 8 consecutive lanes (all 32 lanes call).  par = (s, m) as bf16 bits.
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &par) {
+  float lo = x[0], hi = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  const float r = __fsub_rn(hi, lo);
+  // r / 15 in fp32 is the rounding of the true quotient wherever hi - lo has no error of its own; else through fp64
+  const float quo = diff_err(hi, lo, r) == 0.f ? __fdiv_rn(r, 15.f) : (float)(((double)hi - (double)lo) / 15.0);
+  const float s = __bfloat162float(__float2bfloat16_rn(quo)), m = __bfloat162float(__float2bfloat16_rn(lo));
+  if (!(isfinite(s) && isfinite(m))) {
+    par = 0x7fc07fc0u;
+    return 0u;
+  }
+  par = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
+  if (s == 0.f) return 0u;
+  const float half = 0.5f * s, inv = __fdiv_rn(1.f, s);
+  const bool tiny = s < 1e-30f;   // 1/s may overflow
+  uint32_t word = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = __fsub_rn(x[i], m);
+    float c = rintf(tiny ? __fdiv_rn(a, s) : a * inv);
+    // a * inv may be off by a few units in the last place: where that could have crossed the border between two codes, the
+    // exact remainder (a - c s has no rounding error here) and the error of a decide; a tie goes to the even code
+    const float d = fmaf(-c, s, a);
+    if (fabsf(d) >= half) {
+      const float e = diff_err(x[i], m, a);
+      const bool odd = ((int)c & 1) != 0;
+      if (d > half || (d == half && (e > 0.f || (e == 0.f && odd)))) c += 1.f;
+      else if (d < -half || (d == -half && (e < 0.f || (e == 0.f && odd)))) c -= 1.f;
+    }
+    c = fminf(fmaxf(c, 0.f), 15.f);
+    word |= (uint32_t)(int)c << (4 * i);
+  }
+  return word;
+}
+
+constexpr int kRowsThreads(int hd) { return kKv4Block * hd / 8; }   // 16 tokens of one head
+
+template <typename T, int HD>
+static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_write(Kv4Rows p, bool vec) {
+  typedef Kv4Fmt<HD> F;
+  constexpr int LPR = HD / 8;
+  const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
+  const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
+  const long long slot = tok < p.n ? p.slots[tok] : -1;
+  const bool live = slot >= 0 && slot < p.n_slots;
+  float xk[8] = {}, xv[8] = {};
+  if (live) {
+    load8<T>((const T *)p.k + (size_t)l * p.k_ls + (size_t)tok * p.k_ts + (size_t)head * p.k_hs + 8 * j, vec, xk);
+    load8<T>((const T *)p.v + (size_t)l * p.v_ls + (size_t)tok * p.v_ts + (size_t)head * p.v_hs + 8 * j, vec, xv);
+  }
+  uint32_t pk, pv;
+  const uint32_t wk = quantise8(xk, pk), wv = quantise8(xv, pv);
+  if (!live) return;
+  const long long pg = slot / p.page;
+  const int off = (int)(slot - pg * p.page), t = off % kKv4Block;
+  uint8_t *blk = p.pool + (size_t)l * p.pool_ls + (((size_t)pg * p.H + head) * (p.page / kKv4Block) + off / kKv4Block) * F::kBytes;
+  reinterpret_cast<uint32_t *>(blk + F::KC + t * F::kCodes)[F::key_word(j)] = wk;
+  reinterpret_cast<uint32_t *>(blk + F::VC + t * F::kCodes)[F::val_word(j)] = wv;
+  if ((j & 7) == 0) {
+    reinterpret_cast<uint32_t *>(blk + F::KP + t * F::kPar)[j >> 3] = pk;
+    reinterpret_cast<uint32_t *>(blk + F::VP + t * F::kPar)[j >> 3] = pv;
+  }
+}
+
+// Read: value = s * c + m with one rounding (s * c is exact: 8 + 4 bits), then to T.  Rows whose slot is outside the pool
+// come back as zeros.  Bound by the writes of the unpacked rows.
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t par, float (&x)[8]) {
+  const float s = __uint_as_float(par << 16), m = __uint_as_float(par & 0xffff0000u);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fmaf(s, __uint_as_float(((w >> (4 * i)) & 15u) | 0x4b000000u) - 8388608.f, m);
+}
+
+template <typename T, int HD>
+static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_read(Kv4Rows p, bool vec) {
+  typedef Kv4Fmt<HD> F;
+  constexpr int LPR = HD / 8;
+  const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
+  const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
+  if (tok >= p.n) return;
+  const long long slot = p.slots[tok];
+  float xk[8] = {}, xv[8] = {};
+  if (slot >= 0 && slot < p.n_slots) {
+    const long long pg = slot / p.page;
+    const int off = (int)(slot - pg * p.page), t = off % kKv4Block;
+    const uint8_t *blk = p.pool + (size_t)l * p.pool_ls + (((size_t)pg * p.H + head) * (p.page / kKv4Block) + off / kKv4Block) * F::kBytes;
+    const uint32_t wk = __ldg(reinterpret_cast<const uint32_t *>(blk + F::KC + t * F::kCodes) + F::key_word(j));
+    const uint32_t wv = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VC + t * F::kCodes) + F::val_word(j));
+    const uint32_t pk = __ldg(reinterpret_cast<const uint32_t *>(blk + F::KP + t * F::kPar) + (j >> 3));
+    const uint32_t pv = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VP + t * F::kPar) + (j >> 3));
+    unpack8(wk, pk, xk);
+    unpack8(wv, pv, xv);
+  }
+  store8<T>((T *)p.k + (size_t)l * p.k_ls + (size_t)tok * p.k_ts + (size_t)head * p.k_hs + 8 * j, vec, xk);
+  store8<T>((T *)p.v + (size_t)l * p.v_ls + (size_t)tok * p.v_ts + (size_t)head * p.v_hs + 8 * j, vec, xv);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Attention.  Row i of sequence b (T_b rows, len_b keys) sees keys 0 .. len_b - T_b + i:
+//   q . k_j = sum_g s_jg (q_g . c_jg) + m_jg (sum q_g),      o_g = sum_j (p_j s_jg) c_jg + sum_j p_j m_jg,   p = softmax.
+// Both products run on the tensor cores (m16n8k16, fp16 operands, fp32 accumulation) with the CODES as the 16-row operand
+// and up to 8 query rows as the 8 columns: the parameters are applied to the scores and to the probabilities, never to the
+// codes, so a code costs 5/8 of an instruction: `word & 0x000f000f` is a pair of codes as fp16 subnormals c 2^-24,
+// `word & 0x00f000f0` a pair c 2^-20 (exact; the powers of two are taken back in fp32).  The order of the 64 features of a
+// group in the sum is free, and so is the order of the 16 keys: the storage order of words and the key permutation
+// (row r of the score tile holds key kappa(r), kappa(2t) = t, kappa(2t+1) = t + 4) make every fragment a plain load.
+// fp16 operands.  A query row is multiplied by the power of two that brings its largest element to [2^14, 2^15): a bf16 row
+// is then exact in fp16 down to 2^-24 of its maximum.  The probability times its scale is brought below 2^15 by a power of
+// two from the largest scale seen (raised with an exact rescale of the accumulator, as the running maximum is) and rounded
+// to fp16 -- 11 bits, 3 more than the bf16 result keeps.  Scores, softmax statistics and accumulators are fp32.
+// fp32 inputs.  The tensor core drops the bits that fall below its accumulator's last place, which is a bias, and codes that
+// are all positive make sums that are large against the result: together they would cost an fp32 result five bits.  So the
+// codes enter as c - 8 (fp16 numbers, three instructions a pair; m + 8 s takes the place of m), a query element (and a
+// probability times its scale) is split into a multiple of 16 (11 bits on one grid for the whole row: the products with
+// codes are whole numbers and their sums exact) and an fp16 remainder with an accumulator of its own, 22 bits in all, and
+// the second product's sums over a stage's 32 keys are added to the running output by fp32 additions, which round.
+// Work.  A unit is (layer, key/value head, sequence, tile of 8 NT query rows, chunk of keys); a block of four warps takes
+// a contiguous range of the list of all units (its place in it comes from a prefix sum over the lengths), each warp every
+// fourth 32-key stage of a unit, through its own ring of cp.async stages that runs on across units.  The block joins its
+// warps' results in warp order; rows with several chunks are joined by k_kv4_merge in chunk order.  Chunk boundaries depend
+// on the number of (sequence, head) pairs only and a row's arithmetic on nothing but its own visible keys, so a row comes
+// out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
+// Bound: HBM for few rows (hd 128: 144 bytes a key and head), the mma.sync rate beyond ~16 rows per key/value head.
+constexpr int kAttn4Warps = 4, kAttn4Threads = 32 * kAttn4Warps;
+constexpr int kAttn4Stage = 32;   // keys of a stage
+constexpr int kAttn4Ring = 3;     // stages of a warp's ring
+
+template <int HD, int NT>
+struct Attn4Smem {
+  static constexpr int kStage = 2 * Kv4Fmt<HD>::kBytes;
+  static constexpr int kRing = kAttn4Warps * kAttn4Ring * kStage;
+  static constexpr int kOutLd = HD + 4;                              // outputs, then maximum and denominator
+  static constexpr int kOut = kAttn4Warps * 8 * NT * kOutLd * 4;
+  static constexpr int kFixed = kRing + kOut;                        // + (B + 1) ints
+};
+
+struct Attn4Params {
+  Kv4Attn a;
+  int G, chunk, nch_max;
+  float qk_scale;   // softmax scale * log2(e)
+  bool vec;         // q may be read 16 bytes at a time
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+// x in (-2^15, 2^15) rounded to a multiple of 16: 11 bits on a common grid
+__device__ __forceinline__ float grid16(float x) { return __fsub_rn(__fadd_rn(x, 201326592.f), 201326592.f); }   // 1.5 * 2^27: its unit is 16
+__device__ __forceinline__ float2 half2_vals(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// Lengths of a sequence as the kernels use them: nothing in lens, cu or the table can lead out of the buffers.
+struct Seq4 {
+  int row0, T, len;   // first row, rows, keys present (may exceed the table: positions count from it)
+  int cap;            // keys that can be looked at
+};
+__device__ __forceinline__ Seq4 seq4(const Kv4Attn &a, int b) {
+  Seq4 s;
+  if (a.cu) {
+    s.row0 = min(max(a.cu[b], 0), a.n_rows);
+    s.T = max(min(a.cu[b + 1], a.n_rows) - s.row0, 0);
+  } else {
+    s.row0 = b * a.T;
+    s.T = a.T;
+  }
+  s.len = max(a.lens[b], 0);
+  s.cap = min(s.len, a.max_len);
+  return s;
+}
+__device__ __forceinline__ int seq4_visible(const Seq4 &s, int i) { return min(max(s.len - s.T + i + 1, 0), s.cap); }   // keys that row i sees
+
+// One unit of the list
+struct Unit4 {
+  int b, h, l;          // sequence, key/value head, layer
+  int r0, nrows;        // first row of the tile within the sequence's T * G rows, rows in it
+  int k0, kend;         // keys of this unit: k0 .. kend-1 (empty: kend <= k0)
+  int c, nch;           // chunk, chunks that the tile's rows can see
+  int tok0, T, len, cap;
+};
+
+template <int NT>
+__device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, int x, int y) {
+  Unit4 u;
+  u.b = find_seq(uoff, p.a.B, x);
+  const Seq4 s = seq4(p.a, u.b);
+  u.h = y % p.a.Hkv;
+  u.l = y / p.a.Hkv;
+  const int nchb = max((s.cap + p.chunk - 1) / p.chunk, 1), w = x - uoff[u.b];
+  u.c = w % nchb;
+  u.r0 = (w / nchb) * (8 * NT);
+  u.nrows = min(s.T * p.G - u.r0, 8 * NT);
+  u.tok0 = s.row0; u.T = s.T; u.len = s.len; u.cap = s.cap;
+  const int vis = seq4_visible(s, (u.r0 + u.nrows - 1) / p.G);   // the tile's last row sees most
+  u.nch = max((vis + p.chunk - 1) / p.chunk, 1);
+  u.k0 = u.c * p.chunk;
+  u.kend = min(u.k0 + p.chunk, vis);
+  return u;
+}
+
+// The low (HI = 0: bits 0-3) or high (bits 4-7) codes of the two 16-bit halves of x as an fp16 pair: c 2^-24 / c 2^-20, or
+// c - 8 (0x6400 | n is 1024 + n in fp16).
+template <bool CENTRED, int HI>
+__device__ __forceinline__ uint32_t code_pair(uint32_t x) {
+  uint32_t r = x & (HI ? 0x00f000f0u : 0x000f000fu);
+  if (CENTRED) {
+    r |= 0x64006400u;
+    if (HI) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(r), "r"(0x2c002c00u), "r"(0xd480d480u));   // / 16 - 72
+    else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(0x64086408u));                            // - 1032
+  }
+  return r;
+}
+// (s, m) as stored -> the offset that goes with the codes as code_pair gives them
+template <bool CENTRED>
+__device__ __forceinline__ float code_offset(uint32_t par) {
+  const float m = __uint_as_float(par & 0xffff0000u);
+  return CENTRED ? fmaf(8.f, __uint_as_float(par << 16), m) : m;
+}
+
+template <typename T, int HD, int NT>
+static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_attn(const __grid_constant__ Attn4Params p) {
+  typedef Kv4Fmt<HD> F;
+  typedef Attn4Smem<HD, NT> S;
+  constexpr int NG = F::NG, KS = 4;                       // matrix steps of 16 features per group
+  constexpr int NSP = sizeof(T) == 4 ? 2 : 1;             // fp16 terms of a query element and of a probability
+  constexpr bool CEN = NSP == 2;                          // codes as c - 8
+  constexpr float kLow = CEN ? 1.f : 16777216.f, kHigh = CEN ? 1.f : 1048576.f;   // what a product with a low / high code is multiplied by
+  constexpr float kHighQ = kLow == kHigh ? 1.f : 0.0625f;                         // query elements that meet high codes
+  extern __shared__ __align__(16) unsigned char attn4_sm[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  unsigned char *ring = attn4_sm + warp * kAttn4Ring * S::kStage;
+  float *om = reinterpret_cast<float *>(attn4_sm + S::kRing);
+  int *uoff = reinterpret_cast<int *>(attn4_sm + S::kFixed);
+  const Kv4Attn &a = p.a;
+  pdl_wait();
+
+  // ---- the list of units: exclusive prefix sum over the sequences of (row tiles x chunks) ----
+  {
+    __shared__ int wsum[kAttn4Warps];
+    int carry = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kAttn4Threads) {
+      const int b = b0 + tid;
+      int n = 0;
+      if (b < a.B) {
+        const Seq4 s = seq4(a, b);
+        n = ((s.T * p.G + 8 * NT - 1) / (8 * NT)) * max((s.cap + p.chunk - 1) / p.chunk, 1);
+      }
+      int v = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int z = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += z;
+      }
+      if (lane == 31) wsum[warp] = v;
+      __syncthreads();
+      int before = carry;
+#pragma unroll
+      for (int i = 0; i < kAttn4Warps; ++i) {
+        if (i < warp) before += wsum[i];
+        carry += wsum[i];
+      }
+      if (b < a.B) uoff[b] = before + v - n;
+      __syncthreads();
+    }
+    if (tid == 0) uoff[a.B] = carry;
+    __syncthreads();
+  }
+  const int U = uoff[a.B];
+  const long long total = (long long)U * a.Hkv * a.nl;
+  const long long u0 = total * blockIdx.x / gridDim.x, u1 = total * (blockIdx.x + 1) / gridDim.x;
+  if (u0 >= u1) return;
+
+  // ---- copy side: this warp's stages in order, kAttn4Ring - 1 of them ahead of the arithmetic ----
+  const int bpp = a.page / kKv4Block, page_sh = 31 - __clz(a.page);
+  const size_t page_bytes = (size_t)a.Hkv * bpp * F::kBytes;
+  long long pu = u0;                       // unit
+  int px = (int)(u0 % U), py = (int)(u0 / U), pi = 0, pn = 0, pk0 = 0, pkend = 0;
+  int ent = -1, slot_w = 0;
+  const uint8_t *pbase = nullptr;          // the unit's layer and head within page 0
+  auto enter = [&]() {                     // stages of unit pu, and the page of each of their 16-key blocks (lane 2 i + j: block j of stage i)
+    const Unit4 u = unit4<NT>(p, uoff, px, py);
+    pk0 = u.k0; pkend = u.kend; pi = 0;
+    const int ns = (max(pkend - pk0, 0) + kAttn4Stage - 1) / kAttn4Stage;
+    pn = (ns - warp + kAttn4Warps - 1) / kAttn4Warps;
+    pbase = a.pool + (size_t)u.l * a.pool_ls + (size_t)u.h * bpp * F::kBytes;
+    ent = -1;
+    const int key = pk0 + ((lane >> 1) * kAttn4Warps + warp) * kAttn4Stage + (lane & 1) * kKv4Block;
+    if ((lane >> 1) < pn && key < pkend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
+  };
+  enter();
+  auto copy_next = [&]() {                 // request the next stage (if any); always closes a group
+    while (pi >= pn && pu < u1) {
+      ++pu;
+      if (++px == U) { px = 0; ++py; }
+      if (pu < u1) enter();
+    }
+    if (pu < u1) {
+      unsigned char *dst = ring + slot_w * S::kStage;
+      const int key = pk0 + (pi * kAttn4Warps + warp) * kAttn4Stage;
+      const uint8_t *src[2];
+      bool ok[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int e = __shfl_sync(0xffffffffu, ent, 2 * pi + j);
+        ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
+        src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + (size_t)(((key + 16 * j) & (a.page - 1)) / kKv4Block) * F::kBytes;
+      }
+      constexpr int NC = F::kBytes / 16;             // 16-byte pieces of a block
+#pragma unroll
+      for (int i = 0; i < (2 * NC + 31) / 32; ++i) {
+        const int c = lane + 32 * i, j = c >= NC;
+        if (2 * NC % 32 == 0 || c < 2 * NC) cp_async16(dst + c * 16, (j ? src[1] : src[0]) + (c - j * NC) * 16, j ? ok[1] : ok[0]);
+      }
+      ++pi;
+      slot_w = slot_w + 1 == kAttn4Ring ? 0 : slot_w + 1;
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kAttn4Ring - 1; ++i) copy_next();
+
+  // ---- arithmetic ----
+  int slot_r = 0, cx = (int)(u0 % U), cy = (int)(u0 / U);
+  int q_b = -1, q_y = -1, q_r0 = -1;       // whose query rows the fragments hold
+  uint32_t qf[NT][NSP][NG * KS][2];
+  float qfac[NT][2], qsum[NT][2][NG];      // of this thread's two columns: power-of-two factor with the scale, scaled feature sums
+  for (long long cu = u0; cu < u1; ++cu) {
+    const Unit4 u = unit4<NT>(p, uoff, cx, cy);
+    if (u.b != q_b || cy != q_y || u.r0 != q_r0) {
+      q_b = u.b; q_y = cy; q_r0 = u.r0;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 8 + g;          // fragment column g: row r of the tile
+        float x[NG][16];
+        if (r < u.nrows) {
+          const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
+          const T *src = (const T *)a.q + (size_t)u.l * a.q_ls + (size_t)tok * a.q_ts + (size_t)hq * a.q_hs + 16 * t;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            float y[8];
+            load8<T>(src + n * kKv4Group, p.vec, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[n][i] = y[i];
+            load8<T>(src + n * kKv4Group + 8, p.vec, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[n][8 + i] = y[i];
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < NG; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+        }
+        float top = 0.f, sum[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          sum[n] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) { top = max_nan(top, fabsf(x[n][i])); sum[n] += x[n][i]; }
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+          for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
+        }
+        // power of two that brings the row's largest element to [2^14, 2^15); a row with an infinity or a NaN makes its scores NaN
+        int e = (int)(__float_as_uint(top) >> 23) - 127;
+        const bool odd = e == 128;
+        e = min(max(e, -112), 126);
+        const float f = pow2(14 - e);
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float *y = &x[n][8 * w + 2 * h];   // features 2h, 2h+4 (low code of a byte pair) and 2h+1, 2h+5 (high: c 2^-20)
+              float v[4] = {y[0] * f, y[4] * f, y[1] * f * kHighQ, y[5] * f * kHighQ};
+#pragma unroll
+              for (int sp = 0; sp < NSP; ++sp) {
+                uint32_t (&dst)[2] = qf[nt][sp][n * KS + 2 * w + h];
+                float u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  u[i] = sp + 1 < NSP ? grid16(v[i]) : v[i];
+                  v[i] -= u[i];
+                }
+                dst[0] = half2_bits(u[0], u[1]);
+                dst[1] = half2_bits(u[2], u[3]);
+              }
+            }
+        // scores: fac * (s_0 acc_0 + s_1 acc_1)
+        const float fac = odd ? __uint_as_float(0x7fc00000u) : p.qk_scale * kLow * pow2(e - 14);
+#pragma unroll
+        for (int col = 0; col < 2; ++col) {
+          qfac[nt][col] = __shfl_sync(0xffffffffu, fac, 4 * (2 * t + col));
+#pragma unroll
+          for (int n = 0; n < NG; ++n) qsum[nt][col][n] = __shfl_sync(0xffffffffu, sum[n] * p.qk_scale, 4 * (2 * t + col));
+        }
+      }
+    }
+    int vis[NT][2], vis_min = u.cap;       // keys each of this thread's columns sees
+    const Seq4 sq{u.tok0, u.T, u.len, u.cap};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int col = 0; col < 2; ++col) vis[nt][col] = seq4_visible(sq, (u.r0 + min(nt * 8 + 2 * t + col, u.nrows - 1)) / p.G);
+    vis_min = seq4_visible(sq, u.r0 / p.G);
+
+    float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
+    int E[NG];                              // exponent of the largest value scale so far
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int col = 0; col < 2; ++col) {
+        m[nt][col] = -INFINITY; den[nt][col] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) low[nt][col][n] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < NG; ++n) E[n] = -100;
+
+    const int ns = (max(u.kend - u.k0, 0) + kAttn4Stage - 1) / kAttn4Stage;
+    for (int si = warp; si < ns; si += kAttn4Warps) {
+      const int key0 = u.k0 + si * kAttn4Stage;
+      cp_async_wait<kAttn4Ring - 2>();
+      __syncwarp();    // the stage is there for every lane, and every lane has read the stage before it
+      copy_next();     // ... whose place is filled again
+      const unsigned char *stage = ring + slot_r * S::kStage;
+      slot_r = slot_r + 1 == kAttn4Ring ? 0 : slot_r + 1;
+      const bool edge = key0 + kAttn4Stage > vis_min;   // some row does not see all of the stage
+      const int ka = (g & 1) * 4 + (g >> 1);            // kappa(g): this thread's score rows are keys ka and ka + 8 of a block
+
+      // scores of 2 x 16 keys
+      float sc[NT][2][4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const unsigned char *blk = stage + j * F::kBytes;
+        uint32_t wa[2 * NG], wb[2 * NG], pa[NG], pb[NG];
+        if (NG == 2) {
+          const uint4 va = *reinterpret_cast<const uint4 *>(blk + F::KC + ka * F::kCodes + t * 16);
+          const uint4 vb = *reinterpret_cast<const uint4 *>(blk + F::KC + (ka + 8) * F::kCodes + t * 16);
+          wa[0] = va.x; wa[1] = va.y; wa[2 * NG - 2] = va.z; wa[2 * NG - 1] = va.w;
+          wb[0] = vb.x; wb[1] = vb.y; wb[2 * NG - 2] = vb.z; wb[2 * NG - 1] = vb.w;
+          const uint2 qa = *reinterpret_cast<const uint2 *>(blk + F::KP + ka * F::kPar), qb = *reinterpret_cast<const uint2 *>(blk + F::KP + (ka + 8) * F::kPar);
+          pa[0] = qa.x; pa[NG - 1] = qa.y; pb[0] = qb.x; pb[NG - 1] = qb.y;
+        } else {
+          const uint2 va = *reinterpret_cast<const uint2 *>(blk + F::KC + ka * F::kCodes + t * 8);
+          const uint2 vb = *reinterpret_cast<const uint2 *>(blk + F::KC + (ka + 8) * F::kCodes + t * 8);
+          wa[0] = va.x; wa[1] = va.y; wb[0] = vb.x; wb[1] = vb.y;
+          pa[0] = *reinterpret_cast<const uint32_t *>(blk + F::KP + ka * F::kPar);
+          pb[0] = *reinterpret_cast<const uint32_t *>(blk + F::KP + (ka + 8) * F::kPar);
+        }
+        float d[NT][NSP][NG][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int sp = 0; sp < NSP; ++sp)
+#pragma unroll
+            for (int n = 0; n < NG; ++n) d[nt][sp][n][0] = d[nt][sp][n][1] = d[nt][sp][n][2] = d[nt][sp][n][3] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x = wa[2 * n + w] >> (8 * h), y = wb[2 * n + w] >> (8 * h);
+              const uint32_t a0 = code_pair<CEN, 0>(x), a1 = code_pair<CEN, 0>(y), a2 = code_pair<CEN, 1>(x), a3 = code_pair<CEN, 1>(y);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int sp = 0; sp < NSP; ++sp) mma_f16(d[nt][sp][n], a0, a1, a2, a3, qf[nt][sp][n * KS + 2 * w + h][0], qf[nt][sp][n * KS + 2 * w + h][1]);
+            }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int row = 0; row < 2; ++row)
+#pragma unroll
+            for (int col = 0; col < 2; ++col) {
+              float dot = 0.f, off = 0.f;
+#pragma unroll
+              for (int n = 0; n < NG; ++n) {
+                const uint32_t par = row ? pb[n] : pa[n];
+                dot = fmaf(__uint_as_float(par << 16), NSP == 1 ? d[nt][0][n][2 * row + col] : d[nt][0][n][2 * row + col] + d[nt][NSP - 1][n][2 * row + col], dot);
+                off = fmaf(code_offset<CEN>(par), qsum[nt][col][n], off);
+              }
+              float s = fmaf(qfac[nt][col], dot, off);
+              if (edge && key0 + 16 * j + ka + 8 * row >= vis[nt][col]) s = -INFINITY;
+              sc[nt][j][2 * row + col] = s;
+            }
+      }
+
+      // value parameters of this thread's four keys; keys that no row of the tile sees count as zeros (whatever the page holds there)
+      uint32_t vp[2][2][NG];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int row = 0; row < 2; ++row) {
+          const unsigned char *at = stage + j * F::kBytes + F::VP + (ka + 8 * row) * F::kPar;
+          if (NG == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(at);
+            vp[j][row][0] = v.x; vp[j][row][NG - 1] = v.y;
+          } else {
+            vp[j][row][0] = *reinterpret_cast<const uint32_t *>(at);
+          }
+          if (edge && key0 + 16 * j + ka + 8 * row >= u.kend) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) vp[j][row][n] = 0u;
+          }
+        }
+      // raise E where a finite scale exceeds it
+      bool up = false;
+#pragma unroll
+      for (int n = 0; n < NG; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = (int)((vp[i >> 1][i & 1][n] >> 7) & 0xff) - 127;
+          up = up || (e > E[n] && e != 128);
+        }
+      float grow[NG];
+#pragma unroll
+      for (int n = 0; n < NG; ++n) grow[n] = 1.f;
+      bool rescale = __any_sync(0xffffffffu, up);
+      if (rescale) {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          int e = E[n];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int x = (int)((vp[i >> 1][i & 1][n] >> 7) & 0xff) - 127;
+            if (x != 128) e = max(e, x);
+          }
+          e = __reduce_max_sync(0xffffffffu, e);
+          grow[n] = pow2(max(E[n] - e, -126));
+          E[n] = e;
+        }
+      }
+
+      // running maximum, probabilities
+      float alpha[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int col = 0; col < 2; ++col) {
+          float x = fmaxf(fmaxf(sc[nt][0][col], sc[nt][0][2 + col]), fmaxf(sc[nt][1][col], sc[nt][1][2 + col]));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+          x = fmaxf(x, m[nt][col]);
+          const float ref = x == -INFINITY ? 0.f : x;   // nothing visible yet: every probability below is exp2(-inf) = 0
+          alpha[nt][col] = ex2(m[nt][col] - ref);
+          rescale = rescale || x != m[nt][col];
+          m[nt][col] = x;
+          float sum = 0.f, lo[NG];
+#pragma unroll
+          for (int n = 0; n < NG; ++n) lo[n] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int row = 0; row < 2; ++row) {
+              const float pr = ex2(sc[nt][j][2 * row + col] - ref);
+              sc[nt][j][2 * row + col] = pr;
+              sum += pr;
+#pragma unroll
+              for (int n = 0; n < NG; ++n) {
+                const float add = pr * code_offset<CEN>(vp[j][row][n]);
+                lo[n] += edge && key0 + 16 * j + ka + 8 * row >= vis[nt][col] ? 0.f : add;   // a key that this row does not see may hold a NaN
+              }
+            }
+          den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
+#pragma unroll
+          for (int n = 0; n < NG; ++n) low[nt][col][n] = fmaf(low[nt][col][n], alpha[nt][col], lo[n]);
+        }
+      if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            const float f0 = alpha[nt][0] * grow[n], f1 = alpha[nt][1] * grow[n];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[nt][n * 4 + i][0] *= f0; acc[nt][n * 4 + i][1] *= f1; acc[nt][n * 4 + i][2] *= f0; acc[nt][n * 4 + i][3] *= f1;
+            }
+          }
+      }
+
+      // o += (p s) c
+      uint32_t v[2][4][NG];                  // words of features 8g..8g+7 of the groups, of keys t, t+4, t+8, t+12 of both blocks
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned char *at = stage + j * F::kBytes + F::VC + (t + 4 * i) * F::kCodes + g * 4 * NG;
+          if (NG == 2) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(at);
+            v[j][i][0] = x.x; v[j][i][NG - 1] = x.y;
+          } else {
+            v[j][i][0] = *reinterpret_cast<const uint32_t *>(at);
+          }
+        }
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        uint32_t b[2][NT][NSP][2];
+        const float f = pow2(14 - E[n]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int row = 0; row < 2; ++row) {
+            const float s = __uint_as_float(vp[j][row][n] << 16) * f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float x0 = sc[nt][j][2 * row] * s, x1 = sc[nt][j][2 * row + 1] * s;
+              if (edge) {   // as above: no NaN from a key that the row does not see
+                const int key = key0 + 16 * j + ka + 8 * row;
+                x0 = key >= vis[nt][0] ? 0.f : x0;
+                x1 = key >= vis[nt][1] ? 0.f : x1;
+              }
+              if (NSP == 2) {
+                const float h0 = grid16(x0), h1 = grid16(x1);
+                b[j][nt][0][row] = transpose8(half2_bits(h0, h1));
+                b[j][nt][NSP - 1][row] = transpose8(half2_bits(x0 - h0, x1 - h1));
+              } else {
+                b[j][nt][0][row] = transpose8(half2_bits(x0, x1));
+              }
+            }
+          }
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t fr[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t x = __byte_perm(v[j][0][n], v[j][1][n], hi ? 0x7632 : 0x5410) >> (8 * h);
+              const uint32_t y = __byte_perm(v[j][2][n], v[j][3][n], hi ? 0x7632 : 0x5410) >> (8 * h);
+              fr[j][0] = code_pair<CEN, 0>(x); fr[j][1] = code_pair<CEN, 1>(x); fr[j][2] = code_pair<CEN, 0>(y); fr[j][3] = code_pair<CEN, 1>(y);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float (&o)[4] = acc[nt][n * 4 + 2 * hi + h];
+              if (NSP == 1) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) mma_f16(o, fr[j][0], fr[j][1], fr[j][2], fr[j][3], b[j][nt][0][0], b[j][nt][0][1]);
+              } else {
+                float d[2][4] = {};
+#pragma unroll
+                for (int sp = 0; sp < 2; ++sp)
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) mma_f16(d[sp], fr[j][0], fr[j][1], fr[j][2], fr[j][3], b[j][nt][sp * (NSP - 1)][0], b[j][nt][sp * (NSP - 1)][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += d[0][i] + d[1][i];
+              }
+            }
+          }
+      }
+    }
+
+    // ---- join the four warps ----
+    if (cu != u0) __syncthreads();   // the previous unit's results have been read
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int col = 0; col < 2; ++col) {
+        float l = den[nt][col], lo[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) lo[n] = low[nt][col][n];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+          for (int n = 0; n < NG; ++n) lo[n] += __shfl_xor_sync(0xffffffffu, lo[n], o);
+        }
+        const int r = nt * 8 + 2 * t + col;
+        if (r < u.nrows) {
+          float *dst = om + (size_t)(warp * 8 * NT + r) * S::kOutLd;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes)
+            const float back = pow2(E[n] - 14);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              y[2 * i] = fmaf(acc[nt][n * 4 + i][col] * kLow, back, lo[n]);
+              y[2 * i + 1] = fmaf(acc[nt][n * 4 + i][2 + col] * kHigh, back, lo[n]);
+            }
+            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[0] = make_float4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[1] = make_float4(y[4], y[5], y[6], y[7]);
+          }
+          if (g == 0) { dst[HD] = m[nt][col]; dst[HD + 1] = l; }
+        }
+      }
+    __syncthreads();
+    if (u.c < u.nch) {   // (a chunk that no row of the tile sees leaves nothing behind)
+      const int e = tid % HD;
+      for (int r = tid / HD; r < u.nrows; r += kAttn4Threads / HD) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kAttn4Warps; ++w) M = fmaxf(M, om[(size_t)(w * 8 * NT + r) * S::kOutLd + HD]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float o = 0.f, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttn4Warps; ++w) {
+          const float *src = om + (size_t)(w * 8 * NT + r) * S::kOutLd;
+          const float lw = src[HD + 1], f = lw == 0.f ? 0.f : ex2(src[HD] - ref);   // a warp that saw nothing weighs nothing; a NaN stays
+          if (lw != 0.f) { o = fmaf(f, src[e], o); l = fmaf(f, lw, l); }
+        }
+        const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
+        const size_t row = (size_t)tok * a.Hq + hq;
+        if (u.nch == 1) {
+          ((T *)a.out)[(size_t)u.l * a.o_ls + row * HD + e] = from_f<T>(l == 0.f ? 0.f : o / l);
+        } else {
+          float *dst = a.part + (((size_t)u.l * a.n_rows * a.Hq + row) * p.nch_max + u.c) * (HD + 4);
+          dst[e] = o;
+          if (e == 0) { dst[HD] = M; dst[HD + 1] = l; }
+        }
+      }
+    }
+    if (++cx == U) { cx = 0; ++cy; }
+  }
+  cp_async_wait<0>();
+}
+
+// Joins the chunks of a row in chunk order: four warps take every fourth chunk each, then the warps in order.
+// grid (rows * Hq, layers), 128 threads.
+template <typename T, int HD>
+static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant__ Attn4Params p, int tile) {
+  constexpr int V = HD / 32;
+  __shared__ float so[4][HD], sm[4], sl[4];
+  const Kv4Attn &a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tok = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, l = blockIdx.y;
+  pdl_wait();
+  int b;
+  if (a.cu) {
+    if (tok < a.cu[0] || tok >= a.cu[a.B]) return;   // behind the last sequence
+    b = find_seq(a.cu, a.B, tok);
+  } else {
+    b = tok / a.T;
+  }
+  const Seq4 s = seq4(a, b);
+  const int i = tok - s.row0;
+  if (i < 0 || i >= s.T) return;
+  const int ri = i * p.G + hq % p.G, last = min((ri / tile + 1) * tile, s.T * p.G) - 1;
+  if (seq4_visible(s, last / p.G) <= p.chunk) return;            // the tile had one chunk: its rows are done
+  const int nch = (seq4_visible(s, i) + p.chunk - 1) / p.chunk;
+  const size_t row = (size_t)tok * a.Hq + hq;
+  const float *src = a.part + ((size_t)l * a.n_rows * a.Hq + row) * p.nch_max * (HD + 4);
+  float o[V] = {}, M = -INFINITY, den = 0.f;
+  constexpr int UN = 4;
+  for (int c0 = warp; c0 < nch; c0 += 4 * UN) {
+    float x[UN][V], mc[UN], lc[UN];
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const float *at = src + (size_t)(c0 + 4 * k) * (HD + 4);
+      mc[k] = -INFINITY; lc[k] = 0.f;
+      if (c0 + 4 * k < nch) {
+        mc[k] = __ldcg(at + HD); lc[k] = __ldcg(at + HD + 1);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[k][v] = __ldcg(at + lane + 32 * v);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      if (c0 + 4 * k >= nch || lc[k] == 0.f) continue;
+      const float nm = fmaxf(M, mc[k]), ref = nm == -INFINITY ? 0.f : nm, f = ex2(mc[k] - ref), old = den == 0.f ? 0.f : ex2(M - ref);
+#pragma unroll
+      for (int v = 0; v < V; ++v) o[v] = fmaf(f, x[k][v], o[v] * old);
+      den = fmaf(f, lc[k], den * old);
+      M = nm;
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) so[warp][lane + 32 * v] = o[v];
+  if (lane == 0) { sm[warp] = M; sl[warp] = den; }
+  __syncthreads();
+  if (threadIdx.x < HD) {
+    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), ref = top == -INFINITY ? 0.f : top;
+    float y = 0.f, d = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (sl[w] == 0.f) continue;
+      const float f = ex2(sm[w] - ref);
+      y = fmaf(f, so[w][threadIdx.x], y);
+      d = fmaf(f, sl[w], d);
+    }
+    ((T *)a.out)[(size_t)l * a.o_ls + row * HD + threadIdx.x] = from_f<T>(d == 0.f ? 0.f : y / d);
+  }
+}
+
+}  // namespace snlp

@@ -1,0 +1,58 @@
+// Key/value cache held in 4 bits: launchers shared by the C entry points (kv4.cu) and the model's decode path (snlp.cu).
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace snlp {
+
+constexpr int kKv4Group = 64;        // features that share a scale and a low
+constexpr int kKv4Block = 16;        // tokens of a storage block
+constexpr int kKv4MaxBatch = 4096;   // sequences of one plan or attention call (their prefix sums sit in shared memory)
+
+// Bytes of a storage block: 16 tokens of one head as key codes | key parameters | value codes | value parameters.
+constexpr int kv4_block_bytes(int hd) { return 2 * kKv4Block * (hd / 2 + hd / 16); }
+
+struct Kv4Plan {
+  const int32_t *ctx; int ctx_stride;       // cached tokens of sequence b at ctx[b * ctx_stride]
+  const int32_t *add; int add_const;        // new tokens of sequence b (NULL: add_const each)
+  int B, page;
+  const int32_t *free_pages; int n_free;    // NULL: no page is taken, the table is complete
+  const int32_t *free_head;                 // device, nullable: entries of free_pages already used
+  int32_t *table; int tstride;
+  int max_tokens;
+  int64_t *slots;
+  int32_t *positions, *cu, *lens, *info;    // positions, cu and info nullable
+};
+cudaError_t kv4_plan(const Kv4Plan &p, cudaStream_t st);
+
+struct Kv4Rows {                            // write: src -> pool; read: pool -> src
+  void *k, *v;
+  size_t k_ls, v_ls, k_ts, v_ts, k_hs, v_hs;   // layer / token / head strides in elements
+  uint8_t *pool; size_t pool_ls;               // layer stride in bytes
+  const int64_t *slots;
+  int n, H, hd, page, nl;
+  int64_t n_slots;                             // pages * page size
+  bool fp32;
+};
+cudaError_t kv4_write(const Kv4Rows &p, cudaStream_t st);
+cudaError_t kv4_read(const Kv4Rows &p, cudaStream_t st);
+
+struct Kv4Attn {
+  const void *q; size_t q_ls, q_ts, q_hs;   // elements
+  const uint8_t *pool; size_t pool_ls;      // bytes
+  const int32_t *table; int tstride;
+  const int32_t *lens;                      // keys of sequence b, its new rows' among them
+  const int32_t *cu;                        // [B + 1] first row of every sequence; NULL: T rows each
+  void *out; size_t o_ls;                   // [rows][Hq][hd]
+  float *part;                              // workspace
+  int T, n_rows, B, Hq, Hkv, hd, n_pages, page, max_len, nl;
+  float scale;
+  bool fp32;
+};
+int kv4_chunk(int pairs);                   // keys of a split, from the number of (sequence, key/value head) pairs
+size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl);
+cudaError_t kv4_attention(const Kv4Attn &p, int n_sm, cudaStream_t st);
+cudaError_t kv4_init();                     // kernel attributes of the current device
+
+}  // namespace snlp

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -26,6 +27,7 @@ EXPORTS = [
     "snlp_kv_truncate", "snlp_prefill", "snlp_decode_step", "snlp_decode_step_host", "snlp_draft_and_verify", "snlp_set_flag",
     "snlp_launch_count", "snlp_kernel_times", "snlp_device_status", "snlp_lm_head_greedy_static", "snlp_last_error",
     "snlp_copy_trace", "snlp_draft_and_verify_async", "snlp_graph_count",
+    "snlp_kv4_pool_bytes", "snlp_page_plan", "snlp_kv4_write", "snlp_kv4_read", "snlp_kv4_attention_workspace", "snlp_kv4_attention",
 ]
 
 
@@ -46,6 +48,16 @@ class Solver(C.Structure):
 class Weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("embed", "lm_head", "wqkv", "wo", "wup", "wdn", "hc_res_attn", "hc_res_mlp",
                                           "hc_pre_attn", "hc_pre_mlp", "hc_post_attn", "hc_post_mlp")]
+
+
+class Kv4Pool(C.Structure):
+    _fields_ = [("pages", C.c_void_p)] + [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_head", "head_dim")]
+
+
+class Kv4Attn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("block_table", C.c_void_p), ("lens", C.c_void_p),
+                ("cu_q", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_rows", "B", "n_head", "max_pages", "max_len")] + [("scale", C.c_float)]
 
 
 class SnlpError(RuntimeError):
@@ -312,6 +324,154 @@ def lm_head_greedy_static(hL: torch.Tensor, lm_head_bf16: torch.Tensor, n_stream
     _check(_lib.snlp_lm_head_greedy_static(_ptr(hL), _ptr(lm_head_bf16), C.c_int(rows), C.c_int(n_streams), C.c_int(d),
                                            C.c_int(vocab), C.c_float(rms_eps), _ptr(argmax), _stream()))
     return argmax
+
+
+# -- key/value cache held in 4 bits ------------------------------------------------------------------
+KV4_BLOCK = 16                                   # tokens of a storage block
+_KV4_BLOCK_BYTES = {64: 1152, 128: 2304}         # by head_dim: 16 tokens' codes and parameters, keys and values
+_KV4_HEAD_DIM = {v: k for k, v in _KV4_BLOCK_BYTES.items()}
+
+
+class PagePlan(NamedTuple):
+    """What page_plan leaves behind, all on the device; info = (pages taken, status: 0 = served)."""
+    slots: torch.Tensor
+    positions: torch.Tensor
+    cu_new: torch.Tensor
+    lens: torch.Tensor
+    info: torch.Tensor
+
+
+def _refuse(msg):
+    raise SnlpError(ERR_ARG, msg)
+
+
+_I, _V, _Z = C.c_int, C.c_void_p, C.c_size_t
+_lib.snlp_page_plan.argtypes = [_V, _V, _I, _I, _V, _I, _V, _V, _I, _I, _V, _V, _V, _V, _V, _V]
+_lib.snlp_kv4_write.argtypes = [_V, _V, _V, _I, _V, _V, _I, _V]
+_lib.snlp_kv4_read.argtypes = _lib.snlp_kv4_write.argtypes
+_lib.snlp_kv4_attention_workspace.argtypes = [_V, _V, _V]
+_lib.snlp_kv4_attention.argtypes = [_V, _V, _V, _V, _Z, _V]
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+
+
+def _call_on(index, fn, *args):
+    """fn(*args, stream) with the tensors' device current, on that device's current stream."""
+    if _current_device() == index:
+        rc = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
+    if rc:
+        _check(rc)
+
+
+def _dense_ptr(what, t, dtype, dev):
+    if t.dtype is not dtype or t.device != dev or not t.is_contiguous():
+        _refuse(f"{what} must be a contiguous {dtype} tensor on {dev}")
+    return t.data_ptr()
+
+
+def kv4_pool(n_pages: int, n_kv_head: int, head_dim: int, page_size: int, device="cuda") -> torch.Tensor:
+    """Memory for a pool of pages: uint8 [n_pages, n_kv_head, page_size / 16, block bytes], uninitialised.  The other kv4
+    calls take its geometry from this shape."""
+    if head_dim not in _KV4_BLOCK_BYTES or page_size % KV4_BLOCK:
+        _refuse("head_dim must be 64 or 128, page_size a multiple of 16")
+    return torch.empty((n_pages, n_kv_head, page_size // KV4_BLOCK, _KV4_BLOCK_BYTES[head_dim]), dtype=torch.uint8, device=device)
+
+
+def _kv4_pool_arg(pool):
+    shape = pool.shape
+    if pool.dtype is not torch.uint8 or not pool.is_cuda or len(shape) != 4 or not pool.is_contiguous() or shape[3] not in _KV4_HEAD_DIM:
+        _refuse("pool must be a contiguous cuda uint8 tensor shaped as kv4_pool makes it")
+    n, h, b, size = shape
+    return Kv4Pool(pool.data_ptr(), n, b * KV4_BLOCK, h, _KV4_HEAD_DIM[size])
+
+
+_KV4_DTYPE = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32}
+
+
+def _kv4_dtype(t):
+    if t not in _KV4_DTYPE:
+        _refuse("keys, values and queries are bfloat16 or float32")
+    return _KV4_DTYPE[t]
+
+
+def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, page_size: int, max_tokens: int,
+              free_pages: torch.Tensor | None = None, free_head: torch.Tensor | None = None) -> PagePlan:
+    """Block tables and slot maps from request lengths (snlp_page_plan): int32 cuda tensors ctx_lens, new_lens [B];
+    block_table [B, max_pages] is completed in place with pages from free_pages[free_head:] (None: it has them all).
+    max_tokens: length of the slot map, at least the number of new tokens."""
+    dev, B, shape, i32 = ctx_lens.device, ctx_lens.numel(), block_table.shape, torch.int32
+    if not ctx_lens.is_cuda or len(shape) != 2 or shape[0] != B or new_lens.numel() != B or max_tokens < 0:
+        _refuse("ctx_lens, new_lens [B] and block_table [B, max_pages] must be cuda tensors of one batch, max_tokens >= 0")
+    if free_head is not None and free_head.numel() != 1:
+        _refuse("free_head must be one int32")
+    pc, pn, pt = _dense_ptr("ctx_lens", ctx_lens, i32, dev), _dense_ptr("new_lens", new_lens, i32, dev), _dense_ptr("block_table", block_table, i32, dev)
+    pf, nf = (_dense_ptr("free_pages", free_pages, i32, dev), free_pages.numel()) if free_pages is not None else (None, 0)
+    ph = _dense_ptr("free_head", free_head, i32, dev) if free_head is not None else None
+    slots = ctx_lens.new_empty(max_tokens, dtype=torch.int64)
+    positions, cu, lens, info = ctx_lens.new_empty(max_tokens), ctx_lens.new_empty(B + 1), ctx_lens.new_empty(B), ctx_lens.new_empty(2)
+    _call_on(dev.index, _lib.snlp_page_plan, pc, pn, B, page_size, pf, nf, ph, pt, shape[1], max_tokens, slots.data_ptr(), positions.data_ptr(),
+             cu.data_ptr(), lens.data_ptr(), info.data_ptr())
+    return PagePlan(slots, positions, cu, lens, info)
+
+
+def _kv4_rows(fn, pool, k, v, slots):
+    p, dev, n, dt = _kv4_pool_arg(pool), pool.device, slots.numel(), k.dtype
+    shape = (n, p.n_kv_head, p.head_dim)
+    (kt, kh, ke), (vt, vh, ve) = k.stride() if k.dim() == 3 else (0, 0, 0), v.stride() if v.dim() == 3 else (0, 0, 0)
+    if k.shape != shape or v.shape != shape or k.device != dev or v.device != dev or v.dtype is not dt or (n and (ke != 1 or ve != 1)):
+        _refuse(f"k and v must be {list(shape)} ([tokens, heads, head_dim], one slot per token) of one dtype on the pool's device, features contiguous")
+    _call_on(dev.index, fn, C.byref(p), k.data_ptr(), v.data_ptr(), _kv4_dtype(dt), (C.c_int64 * 4)(kt, kh, vt, vh),
+             _dense_ptr("slots", slots, torch.int64, dev), n)
+
+
+def kv4_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Store k, v [n, n_kv_head, head_dim] (bf16 or fp32, any token and head stride) at int64 slots [n]; tokens whose slot
+    lies outside the pool are left out."""
+    _kv4_rows(_lib.snlp_kv4_write, pool, k, v, slots)
+
+
+def kv4_read(pool: torch.Tensor, slots: torch.Tensor, head_dim: int, dtype=torch.bfloat16, k: torch.Tensor | None = None,
+             v: torch.Tensor | None = None):
+    """(k, v) [n, n_kv_head, head_dim] of the tokens at int64 slots [n]; zeros where a slot lies outside the pool."""
+    if k is None or v is None:
+        shape = (slots.numel(), pool.shape[1], head_dim)
+        k = pool.new_empty(shape, dtype=dtype) if k is None else k
+        v = pool.new_empty(shape, dtype=dtype) if v is None else v
+    _kv4_rows(_lib.snlp_kv4_read, pool, k, v, slots)
+    return k, v
+
+
+def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor | None = None,
+                  max_len: int = 0, scale: float | None = None, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention of q [rows, n_head, head_dim] over the pages (snlp_kv4_attention): int32 block_table [B, max_pages],
+    lens [B]; cu_q [B + 1] gives each sequence's rows (None: rows / B each).  max_len: a bound of the lengths known on the
+    host (0: the table's capacity); workspace: uint8, by default allocated per call."""
+    p, dev, shape, B, tab, i32 = _kv4_pool_arg(pool), pool.device, q.shape, lens.numel(), block_table.shape, torch.int32
+    if q.device != dev or len(shape) != 3 or shape[2] != p.head_dim or (shape[0] and q.stride(2) != 1):
+        _refuse("q must be [rows, n_head, head_dim] on the pool's device, features contiguous")
+    if len(tab) != 2 or tab[0] != B or (cu_q is not None and cu_q.numel() != B + 1):
+        _refuse("block_table must be [B, max_pages], lens [B], cu_q [B + 1]")
+    if out is None:
+        out = q.new_empty(shape)
+    elif out.shape != shape:
+        _refuse("out must have q's shape")
+    qt, qh, _ = q.stride()
+    a = Kv4Attn(q.data_ptr(), qt, qh, _dense_ptr("block_table", block_table, i32, dev), _dense_ptr("lens", lens, i32, dev),
+                _dense_ptr("cu_q", cu_q, i32, dev) if cu_q is not None else None, _kv4_dtype(q.dtype), shape[0], B, shape[1], tab[1], max_len,
+                scale if scale is not None else 0.0)
+    po = _dense_ptr("out", out, q.dtype, dev)
+    pp, pa, pw, size = C.byref(p), C.byref(a), None, 0
+    if workspace is None:
+        need = C.c_size_t()
+        _check(_lib.snlp_kv4_attention_workspace(pp, pa, C.byref(need)))
+        if need.value:
+            workspace = pool.new_empty(need.value)
+    if workspace is not None:
+        pw, size = _dense_ptr("workspace", workspace, torch.uint8, dev), workspace.numel()
+    _call_on(dev.index, _lib.snlp_kv4_attention, pp, pa, po, pw, size)
+    return out
 
 
 def raw_library() -> C.CDLL:
