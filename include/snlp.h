@@ -170,6 +170,13 @@ int snlp_lm_head(snlp_model *m, const float *hL, int rows, float *logits, int32_
  * A cache may outlive its model (snlp_destroy leaves it valid for snlp_kv_destroy only).
  * Errors: ARG, SHAPE (B > max_batch, max_ctx > config.max_ctx), OOM. */
 int snlp_kv_create(snlp_model *m, int B, int max_ctx, snlp_kv **out);
+/* The same cache held in 4 bits (format: "key/value cache held in 4 bits" below; head_dim 64 or 128; at 128 a token, head and
+ * layer takes 144 bytes instead of 512): every call that takes a cache takes this one too.  New keys and values are rounded to
+ * 4 bits before any query sees them, so K = L sweeps still equal sequential execution and a verify block the decode steps it
+ * checks.  For prompts of bf16 models it keeps one layer's rows in bf16 beside it; a cache made before the weights are loaded
+ * does without and takes longer over prompts.
+ * Errors: ARG, SHAPE (B > max_batch or 4096, max_ctx > config.max_ctx), UNSUPPORTED (head_dim), OOM, CUDA. */
+int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **out);
 int snlp_kv_destroy(snlp_kv *kv);
 /* The length is kept on the device and mirrored on the host.  After snlp_draft_and_verify_async the host knows only an
  * upper bound; snlp_kv_len (and snlp_kv_truncate) then wait for the device (cudaDeviceSynchronize) and read the length

@@ -144,24 +144,24 @@ __global__ void __launch_bounds__(256) k_gemm_nt(const T *__restrict__ A, size_t
 
 // ---------------------------------------------------------------------------------------------
 // Rotary + QK-norm + scatter.  Reads raw projections qkv[l][row][3d]; writes q[l][row][d] and the
-// layer's key/value slots at position *pos_base + (row % T) of sequence row / T.
+// layer's key/value slots at position *pos_base + (row % T) of sequence row / T (kv_local: at row % T, a staging area).
 // grid (rows, 3H, nl), 128 threads.  rope_cs[pos][hd/2] holds (cos, sin) pairs.
 template <typename T>
 __global__ void k_rope_qknorm_store(const float *__restrict__ qkv, size_t qkv_ls, T *__restrict__ q, size_t q_ls,
                                     T *__restrict__ kc, T *__restrict__ vc, size_t kv_ls, size_t kv_bs, int Tlen, int H,
-                                    int hd, const int *__restrict__ pos_base, const float2 *__restrict__ rope_cs, float eps) {
+                                    int hd, const int *__restrict__ pos_base, const float2 *__restrict__ rope_cs, float eps, int kv_local) {
   __shared__ float red[32];
   const int row = blockIdx.x, hh = blockIdx.y, l = blockIdx.z;
   const int d = H * hd, kind = hh / H, head = hh % H, half = hd >> 1;
-  const int b = row / Tlen, pos = *pos_base + (row % Tlen);
+  const int b = row / Tlen, pos = *pos_base + (row % Tlen), kv_row = kv_local ? row % Tlen : pos;
   const float *src = qkv + (size_t)l * qkv_ls + (size_t)row * 3 * d + (size_t)kind * d + (size_t)head * hd;
   if (kind == 2) {
-    T *dst = vc + (size_t)l * kv_ls + (size_t)b * kv_bs + (size_t)pos * d + (size_t)head * hd;
+    T *dst = vc + (size_t)l * kv_ls + (size_t)b * kv_bs + (size_t)kv_row * d + (size_t)head * hd;
     for (int i = threadIdx.x; i < hd; i += blockDim.x) dst[i] = from_f<T>(src[i]);
     return;
   }
   T *dst = kind == 0 ? q + (size_t)l * q_ls + (size_t)row * d + (size_t)head * hd
-                     : kc + (size_t)l * kv_ls + (size_t)b * kv_bs + (size_t)pos * d + (size_t)head * hd;
+                     : kc + (size_t)l * kv_ls + (size_t)b * kv_bs + (size_t)kv_row * d + (size_t)head * hd;
   // hd <= 256 and blockDim = 128, so each thread owns at most one rotary pair
   float y1 = 0.f, y2 = 0.f;
   const int i = threadIdx.x;

@@ -56,6 +56,8 @@ static int chunks_max(int B, int Hkv, int max_len) {
   return (int)(((int64_t)max_len + c - 1) / c);
 }
 
+int kv4_attention_launches(int B, int Hkv, int max_len) { return chunks_max(B, Hkv, max_len) > 1 ? 2 : 1; }
+
 size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl) {
   const int n = chunks_max(B, Hkv, max_len);
   return n < 2 ? 0 : (size_t)nl * n_rows * Hq * n * (hd + 4) * sizeof(float);

@@ -270,7 +270,7 @@ static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_write(Kv4Rows p
   constexpr int LPR = HD / 8;
   const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
   const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
-  const long long slot = tok < p.n ? p.slots[tok] : -1;
+  const long long slot = tok < p.n ? p.slots[(size_t)l * p.slots_ls + tok] : -1;
   const bool live = slot >= 0 && slot < p.n_slots;
   float xk[8] = {}, xv[8] = {};
   if (live) {
@@ -306,7 +306,7 @@ static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_read(Kv4Rows p,
   const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
   const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
   if (tok >= p.n) return;
-  const long long slot = p.slots[tok];
+  const long long slot = p.slots[(size_t)l * p.slots_ls + tok];
   float xk[8] = {}, xv[8] = {};
   if (slot >= 0 && slot < p.n_slots) {
     const long long pg = slot / p.page;

@@ -30,7 +30,7 @@ struct Kv4Rows {                            // write: src -> pool; read: pool ->
   void *k, *v;
   size_t k_ls, v_ls, k_ts, v_ts, k_hs, v_hs;   // layer / token / head strides in elements
   uint8_t *pool; size_t pool_ls;               // layer stride in bytes
-  const int64_t *slots;
+  const int64_t *slots; size_t slots_ls;       // slots of layer l at slots + l * slots_ls
   int n, H, hd, page, nl;
   int64_t n_slots;                             // pages * page size
   bool fp32;
@@ -53,6 +53,7 @@ struct Kv4Attn {
 int kv4_chunk(int pairs);                   // keys of a split, from the number of (sequence, key/value head) pairs
 size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl);
 cudaError_t kv4_attention(const Kv4Attn &p, int n_sm, cudaStream_t st);
+int kv4_attention_launches(int B, int Hkv, int max_len);   // kernels of one call
 cudaError_t kv4_init();                     // kernel attributes of the current device
 
 }  // namespace snlp

@@ -19,6 +19,7 @@
 #include "correct.cuh"
 #include "decode.cuh"
 #include "generic.cuh"
+#include "kv4.h"
 #include "umma_gemm.cuh"
 #include "umma_gemm2.cuh"
 #include "umma_chain.cuh"
@@ -62,6 +63,7 @@ void set_last_error(const char *msg) { g_err = msg; }  // for the library's othe
 // handles
 constexpr size_t kCorrExtraSmem = 32768;   // k_correct: shared memory beyond the operand ring (norm partials, staged coefficients)
 constexpr int kMaxSplits = 4;    // K-splits of the partial-sum GEMV outputs
+constexpr int kKv4Page = 64;     // tokens of a page of a model's 4-bit cache
 constexpr int kDecodeRows = 16;  // largest row count served by the decode-regime kernels
 constexpr size_t kCorrSmallSmem = 160 * 1024;
 
@@ -140,7 +142,14 @@ struct snlp_kv {
   // round only an upper bound is known here (len_known == false, len_hi) until snlp_kv_len reads the device value.
   int len = 0, len_hi = 0;
   bool len_known = true;
-  void *k = nullptr, *v = nullptr;
+  void *k = nullptr, *v = nullptr;   // 4-bit cache: one layer's keys / values unpacked for the prompt attention (NULL where that kernel does not serve the model)
+  // 4-bit cache (pool != NULL): per layer a pool of pages; block table and slots are the same for every layer
+  uint8_t *pool = nullptr;
+  size_t pool_ls = 0;                // bytes of a layer's pool
+  int n_pages = 0, row_pages = 0;    // pages of a layer, of a sequence
+  int32_t *table = nullptr, *lens = nullptr;   // [B][row_pages]; [B] lengths with the call's new tokens
+  int64_t *slots = nullptr, *all_slots = nullptr;   // [max_rows] of the call's new tokens; [B][max_ctx] of every position
+  float *part = nullptr;             // workspace of a single layer's attention
   int *pos = nullptr;   // device int[4]: [0] the length, [1] the length saved at the start of a draft-and-verify round
 };
 
@@ -152,6 +161,7 @@ struct Fwd {
   const int *pos;       // device: first position of this call
   int pos_hi;           // host copy of *pos
   int kv_rows;          // rows per sequence in the key / value store
+  snlp_kv *kv4 = nullptr;   // 4-bit cache: kc / vc are a staging area for the call's own rows, which kv4_store puts into the pages
   const int32_t *embed_ids = nullptr;   // non-NULL: state 0 is the embedding of these tokens and has not been written yet
   const int32_t *const *embed_ids_pp = nullptr;   // the same, with the tokens' address read from a device slot
   bool last_pass = false;   // no sweep follows this correction: it need not prepare the next sweep's branch inputs
@@ -600,6 +610,89 @@ static int correct(snlp_model *m, const Fwd &f, int l0, int nsteps, int lstep, i
   return SNLP_OK;
 }
 
+// Tensor-core attention: 128-query items over the (layer, sequence, head, query tile) grid, persistent CTAs.
+static int prompt_attention(snlp_model *m, const Fwd &f, const __nv_bfloat16 *q, const __nv_bfloat16 *kc, const __nv_bfloat16 *vc, size_t kv_ls,
+                            size_t kv_bs, int kv_rows, __nv_bfloat16 *att, int nl) {
+  const int M = f.M, d = m->cfg.d_model, H = m->cfg.n_head;
+  const size_t Md = (size_t)M * d;
+  CUtensorMap tq, tk, tv, to;
+  if (!make_tmap_bf16(m->encode_tiled, &tq, q, d, M, nl, Md, kFuTile) ||
+      !make_tmap_kv(m->encode_tiled, &tk, kc, d, kv_rows, f.B, nl, kv_bs, kv_ls) ||
+      !make_tmap_kv(m->encode_tiled, &tv, vc, d, kv_rows, f.B, nl, kv_bs, kv_ls) ||
+      !make_tmap_kv(m->encode_tiled, &to, att, d, f.T, f.B, nl, (size_t)f.T * d, Md))
+    return fail(SNLP_ERR_CUDA, "cuTensorMapEncodeTiled failed for the attention operands");
+  FaUmmaParams ap{};
+  ap.T = f.T; ap.H = H; ap.BH = f.B * H; ap.nq = (f.T + kFuTile - 1) / kFuTile;
+  ap.n_items = ap.nq * ap.BH * nl; ap.pos_base = f.pos; ap.err = m->dev_err;
+  const int grid = ap.n_items < m->n_sm ? ap.n_items : m->n_sm;
+  KLAUNCH(m, f.st, KC_ATTN, k_attn_umma<<<grid, kFuThreads, kFuSmem, f.st>>>(tq, tk, tv, to, ap, nl));
+  return SNLP_OK;
+}
+
+// ---- 4-bit cache ----
+static int kv4_check(cudaError_t e) { return e == cudaSuccess ? SNLP_OK : fail(SNLP_ERR_CUDA, "kernel launch failed (4-bit cache): %s", cudaGetErrorString(e)); }
+
+// Slots and lengths of the call's new tokens, once per call (the block table is complete since the cache's creation).
+static int kv4_begin(snlp_model *m, const Fwd &f) {
+  snlp_kv *kv = f.kv4;
+  Kv4Plan p{};
+  p.ctx = f.pos; p.ctx_stride = 0; p.add_const = f.T; p.B = f.B; p.page = kKv4Page;
+  p.table = kv->table; p.tstride = kv->row_pages; p.max_tokens = f.M; p.slots = kv->slots; p.lens = kv->lens;
+  TimedLaunch tl_(m, f.st, KC_OTHER);
+  return kv4_check(kv4_plan(p, f.st));
+}
+
+static Kv4Rows kv4_rows(snlp_model *m, const Fwd &f, int l0) {
+  const snlp_config &c = m->cfg;
+  Kv4Rows p{};
+  p.pool = f.kv4->pool + (size_t)l0 * f.kv4->pool_ls; p.pool_ls = f.kv4->pool_ls;
+  p.H = c.n_head; p.hd = c.head_dim; p.page = kKv4Page; p.n_slots = (int64_t)f.kv4->n_pages * kKv4Page; p.fp32 = c.dtype == SNLP_DTYPE_FP32;
+  p.k_ts = p.v_ts = c.d_model; p.k_hs = p.v_hs = c.head_dim;
+  return p;
+}
+
+// the staged keys and values of layers l0 .. l0+nl-1 into their pages
+static int kv4_store(snlp_model *m, const Fwd &f, int l0, int nl) {
+  Kv4Rows p = kv4_rows(m, f, l0);
+  p.k = (char *)f.kc + (size_t)l0 * f.kv_ls * m->esz; p.v = (char *)f.vc + (size_t)l0 * f.kv_ls * m->esz;
+  p.k_ls = p.v_ls = f.kv_ls; p.slots = f.kv4->slots; p.n = f.M; p.nl = nl;
+  TimedLaunch tl_(m, f.st, KC_OTHER);
+  return kv4_check(kv4_write(p, f.st));
+}
+
+// Layer l's positions so far, of every sequence, as bf16 rows [B][max_ctx][d].  The host's upper bound of the length counts: what
+// lies beyond the length is zeros or older rows, which the causal attention gives no weight.
+static int kv4_unpack(snlp_model *m, const Fwd &f, int l) {
+  Kv4Rows p = kv4_rows(m, f, l);
+  p.k = f.kv4->k; p.v = f.kv4->v; p.k_ls = p.v_ls = (size_t)f.kv4->max_ctx * m->cfg.d_model;
+  p.pool_ls = 0; p.slots = f.kv4->all_slots; p.slots_ls = f.kv4->max_ctx;   // the "layers" of this launch are the sequences
+  p.n = std::min(f.pos_hi + f.T, f.kv4->max_ctx); p.nl = f.B;
+  TimedLaunch tl_(m, f.st, KC_OTHER);
+  return kv4_check(kv4_read(p, f.st));
+}
+
+// attention of layers l0 .. l0+nl-1 straight from the pages
+static int kv4_attend(snlp_model *m, const Fwd &f, int l0, int nl, const void *q, void *att) {
+  const snlp_config &c = m->cfg;
+  const size_t Md = (size_t)f.M * c.d_model;
+  Kv4Attn a{};
+  a.q_ls = Md; a.q_ts = c.d_model; a.q_hs = c.head_dim; a.o_ls = Md;
+  a.pool_ls = f.kv4->pool_ls; a.table = f.kv4->table; a.tstride = f.kv4->row_pages; a.lens = f.kv4->lens;
+  a.T = f.T; a.n_rows = f.M; a.B = f.B; a.Hq = a.Hkv = c.n_head; a.hd = c.head_dim; a.n_pages = f.kv4->n_pages; a.page = kKv4Page;
+  a.max_len = f.kv4->max_ctx; a.scale = 1.f / std::sqrt((float)c.head_dim); a.fp32 = c.dtype == SNLP_DTYPE_FP32;
+  // the decode regime has workspace for all layers at once; more rows go layer by layer
+  const bool all = f.M <= kDecodeRows;
+  for (int i = 0; i < nl; i += all ? nl : 1) {
+    a.q = (const char *)q + i * Md * m->esz; a.out = (char *)att + i * Md * m->esz;
+    a.pool = f.kv4->pool + (size_t)(l0 + i) * f.kv4->pool_ls;
+    a.part = all ? m->attn_part : f.kv4->part; a.nl = all ? nl : 1;
+    TimedLaunch tl_(m, f.st, KC_ATTN);
+    count(m, kv4_attention_launches(f.B, c.n_head, a.max_len) - 1);
+    TRY(kv4_check(kv4_attention(a, m->n_sm, f.st)));
+  }
+  return SNLP_OK;
+}
+
 // Blocks l0 .. l0+nl-1 (branch outputs a, m; the correction is separate).  fuse == 1: each block on its own current
 // input state.  fuse > 1: fused chunks (App. C.3): the layers of a chunk read the chunk's input; the per-layer
 // attention outputs a[l] are summed by the consumer (a_splits = fuse), likewise the MLP outputs.
@@ -623,8 +716,13 @@ static int blocks_generic(snlp_model *m, const Fwd &f, int l0, int nl, int fuse)
     KLAUNCH(m, st, KC_OTHER, k_rmsnorm_cast<T><<<dim3(M, nin), 256, 0, st>>>(xa_src, Md, (size_t)d, 1, xn, Md, d, c.rms_eps));
     TRY(gemm<T>(m, st, KC_QKV, xn, in_ls, (const T *)m->wqkv + (size_t)h0 * 3 * d * d, (size_t)3 * d * d, qkv, (size_t)M * 3 * d, M, 3 * d, d, g));
     KLAUNCH(m, st, KC_OTHER, k_rope_qknorm_store<T><<<dim3(M, 3 * H, g), 128, 0, st>>>(qkv, (size_t)M * 3 * d, q, Md, kc, vc, f.kv_ls, f.kv_bs, f.T, H, hd, f.pos,
-                                                               m->rope, c.rms_eps));
-    KLAUNCH(m, st, KC_ATTN, k_attn_generic<T><<<dim3((M * H + 3) / 4, g), 128, 0, st>>>(q, Md, kc, vc, f.kv_ls, f.kv_bs, att, Md, M, f.T, H, hd, f.pos));
+                                                               m->rope, c.rms_eps, f.kv4 ? 1 : 0));
+    if (f.kv4) {
+      TRY(kv4_store(m, f, h0, g));
+      TRY(kv4_attend(m, f, h0, g, q, att));
+    } else {
+      KLAUNCH(m, st, KC_ATTN, k_attn_generic<T><<<dim3((M * H + 3) / 4, g), 128, 0, st>>>(q, Md, kc, vc, f.kv_ls, f.kv_bs, att, Md, M, f.T, H, hd, f.pos));
+    }
     TRY(gemm<T>(m, st, KC_OPROJ, att, Md, (const T *)m->wo + (size_t)h0 * d * d, (size_t)d * d, a, Md, M, d, d, g));
     KLAUNCH(m, st, KC_OTHER, k_resid_rmsnorm_cast<T><<<dim3(M, nin), 256, 0, st>>>(xm_src, Md, (size_t)d, a, Md, fuse > 1 ? fuse : 1, Md, m->coef, h0, xn, Md, d,
                                                                 c.rms_eps));
@@ -819,9 +917,20 @@ static int blocks_umma(snlp_model *m, const Fwd &f, int l0, int nl, int fuse) {
     p.q = q; p.q_ls = Md; p.kc = kc; p.vc = vc; p.kv_ls = f.kv_ls; p.kv_bs = f.kv_bs;
     p.T = f.T; p.d = d; p.pos_base = f.pos; p.rope = m->rope; p.rope_t = m->rope_t; p.rope_ld = c.max_ctx; p.qk_eps = c.rms_eps;
     p.a_share = fuse;
+    p.kv_local = f.kv4 ? 1 : 0;
     TRY(umma_gemm<UEPI_QKV>(m, st, KC_QKV, xb, Md, m->w_qkv, l0, p, M, 3 * d, d, 1, nl));
   }
-  if (small) {
+  if (f.kv4) TRY(kv4_store(m, f, l0, nl));
+  if (f.kv4 && (f.T <= kDecodeRows || !f.kv4->k)) {
+    TRY(kv4_attend(m, f, l0, nl, q, att));
+  } else if (f.kv4) {
+    // a prompt chunk: layer by layer, the sequences' positions so far are unpacked for the tensor-core prompt attention
+    for (int i = 0; i < nl; ++i) {
+      TRY(kv4_unpack(m, f, l0 + i));
+      TRY(prompt_attention(m, f, q + i * Md, (const T *)f.kv4->k, (const T *)f.kv4->v, (size_t)f.B * f.kv4->max_ctx * d, (size_t)f.kv4->max_ctx * d,
+                           f.kv4->max_ctx, att + i * Md, 1));
+    }
+  } else if (small) {
     const int csub = attn_csub(f.B * H);
     const int nchunk = (f.pos_hi + f.T - 1) / (csub * kAttnSub) + 1;
     // Where the chunk partials are merged.  In the attention kernel itself the CTA that arrives last at its (layer,
@@ -836,18 +945,7 @@ static int blocks_umma(snlp_model *m, const Fwd &f, int l0, int nl, int fuse) {
                                        comb ? 0 : 1));
     comb_nchunk = nchunk;
   } else {
-    // tensor-core attention: 128-query items over the (layer, sequence, head, query tile) grid, persistent CTAs
-    CUtensorMap tq, tk, tv, to;
-    if (!make_tmap_bf16(m->encode_tiled, &tq, q, d, M, nl, Md, kFuTile) ||
-        !make_tmap_kv(m->encode_tiled, &tk, kc, d, f.kv_rows, f.B, nl, f.kv_bs, f.kv_ls) ||
-        !make_tmap_kv(m->encode_tiled, &tv, vc, d, f.kv_rows, f.B, nl, f.kv_bs, f.kv_ls) ||
-        !make_tmap_kv(m->encode_tiled, &to, att, d, f.T, f.B, nl, (size_t)f.T * d, Md))
-      return fail(SNLP_ERR_CUDA, "cuTensorMapEncodeTiled failed for the attention operands");
-    FaUmmaParams ap{};
-    ap.T = f.T; ap.H = H; ap.BH = f.B * H; ap.nq = (f.T + kFuTile - 1) / kFuTile;
-    ap.n_items = ap.nq * ap.BH * nl; ap.pos_base = f.pos; ap.err = m->dev_err;
-    const int grid = ap.n_items < m->n_sm ? ap.n_items : m->n_sm;
-    KLAUNCH(m, st, KC_ATTN, k_attn_umma<<<grid, kFuThreads, kFuSmem, st>>>(tq, tk, tv, to, ap, nl));
+    TRY(prompt_attention(m, f, q, kc, vc, f.kv_ls, f.kv_bs, f.kv_rows, att, nl));
   }
   UmmaParams po{}, pu{}, pd{};
   po.c = a; po.z = ub; po.out_ls = Md;
@@ -971,6 +1069,7 @@ static int solve(snlp_model *m, const Fwd &f, const snlp_solver &sol, float *res
   const snlp_config &c = m->cfg;
   const int L = c.n_layer, F = sol.fuse;
   const bool seq = sol.mode == SNLP_MODE_SEQUENTIAL;
+  if (f.kv4) TRY(kv4_begin(m, f));
   const int S = (seq && F == 1) ? L : sol.prefix;
   // a decode step hands over token ids instead of state 0: the initialisation kernel embeds them itself where it runs
   // on state 0; every other path needs the embedding first
@@ -1233,6 +1332,11 @@ extern "C" int snlp_copy_trace(snlp_model *m, int rows, float *trace_out, void *
   return SNLP_OK;
 }
 
+static void kv_free(snlp_kv *kv) {
+  for (void *p : {kv->k, kv->v, (void *)kv->pos, (void *)kv->pool, (void *)kv->table, (void *)kv->lens, (void *)kv->slots, (void *)kv->all_slots, (void *)kv->part}) cudaFree(p);
+  delete kv;
+}
+
 extern "C" int snlp_kv_create(snlp_model *m, int B, int max_ctx, snlp_kv **out) {
   if (!m || !out) return fail(SNLP_ERR_ARG, "snlp_kv_create: NULL argument");
   if (B < 1 || max_ctx < 1) return fail(SNLP_ERR_ARG, "snlp_kv_create: B and max_ctx must be >= 1");
@@ -1258,6 +1362,55 @@ extern "C" int snlp_kv_create(snlp_model *m, int B, int max_ctx, snlp_kv **out) 
   return SNLP_OK;
 }
 
+extern "C" int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **out) {
+  if (!m || !out) return fail(SNLP_ERR_ARG, "snlp_kv_create_4bit: NULL argument");
+  const snlp_config &c = m->cfg;
+  if (B < 1 || max_ctx < 1) return fail(SNLP_ERR_ARG, "snlp_kv_create_4bit: B and max_ctx must be >= 1");
+  if (B > c.max_batch || B > kKv4MaxBatch) return fail(SNLP_ERR_SHAPE, "snlp_kv_create_4bit: B = %d exceeds %d", B, std::min(c.max_batch, kKv4MaxBatch));
+  if (max_ctx > c.max_ctx) return fail(SNLP_ERR_SHAPE, "snlp_kv_create_4bit: max_ctx = %d exceeds the model's %d", max_ctx, c.max_ctx);
+  if (c.head_dim != 64 && c.head_dim != 128) return fail(SNLP_ERR_UNSUPPORTED, "snlp_kv_create_4bit: head_dim must be 64 or 128 (got %d)", c.head_dim);
+  snlp_kv *kv = new (std::nothrow) snlp_kv;
+  if (!kv) return fail(SNLP_ERR_OOM, "snlp_kv_create_4bit: host allocation failed");
+  kv->m = m; kv->B = B; kv->max_ctx = max_ctx;
+  kv->row_pages = (max_ctx + kKv4Page - 1) / kKv4Page;
+  kv->n_pages = B * kv->row_pages;
+  kv->pool_ls = (size_t)kv->n_pages * c.n_head * (kKv4Page / kKv4Block) * kv4_block_bytes(c.head_dim);
+  const size_t pool = c.n_layer * kv->pool_ls;
+  const bool prompts = m->have_wmaps && c.dtype == SNLP_DTYPE_BF16 && c.head_dim == 128;   // the tensor-core prompt attention serves this model
+  const size_t dense = prompts ? (size_t)B * max_ctx * c.d_model * m->esz : 0;
+  const size_t part = kv4_workspace(c.max_rows, B, c.n_head, c.n_head, c.head_dim, max_ctx, 1);
+  bool ok = cudaMalloc((void **)&kv->pool, pool) == cudaSuccess && cudaMalloc((void **)&kv->table, (size_t)kv->n_pages * 4) == cudaSuccess &&
+            cudaMalloc((void **)&kv->lens, (size_t)B * 4) == cudaSuccess && cudaMalloc((void **)&kv->slots, (size_t)c.max_rows * 8) == cudaSuccess &&
+            cudaMalloc((void **)&kv->all_slots, (size_t)B * max_ctx * 8) == cudaSuccess && cudaMalloc((void **)&kv->pos, 16) == cudaSuccess &&
+            (dense == 0 || (cudaMalloc(&kv->k, dense) == cudaSuccess && cudaMalloc(&kv->v, dense) == cudaSuccess)) &&
+            (part == 0 || cudaMalloc((void **)&kv->part, part) == cudaSuccess);
+  if (!ok) {
+    cudaGetLastError();
+    kv_free(kv);
+    return fail(SNLP_ERR_OOM, "snlp_kv_create_4bit: cudaMalloc of %zu bytes failed", pool + 2 * dense + part);
+  }
+  // the table gives sequence b the pages b * row_pages ..; a page that was never written holds zeros, so that nothing read
+  // beyond a length is a NaN
+  std::vector<int32_t> table(kv->n_pages);
+  std::vector<int64_t> slots((size_t)B * max_ctx);
+  std::iota(table.begin(), table.end(), 0);
+  for (int b = 0; b < B; ++b)
+    for (int p = 0; p < max_ctx; ++p) slots[(size_t)b * max_ctx + p] = (int64_t)b * kv->row_pages * kKv4Page + p;
+  ok = cudaMemset(kv->pool, 0, pool) == cudaSuccess && cudaMemset(kv->pos, 0, 16) == cudaSuccess &&
+       cudaMemcpy(kv->table, table.data(), table.size() * 4, cudaMemcpyHostToDevice) == cudaSuccess &&
+       cudaMemcpy(kv->all_slots, slots.data(), slots.size() * 8, cudaMemcpyHostToDevice) == cudaSuccess;
+  if (ok && dense) ok = cudaMemset(kv->k, 0, dense) == cudaSuccess && cudaMemset(kv->v, 0, dense) == cudaSuccess;
+  if (ok) ok = kv4_init() == cudaSuccess;
+  if (!ok) {
+    cudaGetLastError();
+    kv_free(kv);
+    return fail(SNLP_ERR_CUDA, "snlp_kv_create_4bit: initialisation failed");
+  }
+  m->caches.push_back(kv);
+  *out = kv;
+  return SNLP_OK;
+}
+
 extern "C" int snlp_kv_destroy(snlp_kv *kv) {
   if (!kv) return fail(SNLP_ERR_ARG, "snlp_kv_destroy: NULL handle");
   cudaDeviceSynchronize();
@@ -1268,8 +1421,7 @@ extern "C" int snlp_kv_destroy(snlp_kv *kv) {
     }
     kv->m->caches.erase(std::remove(kv->m->caches.begin(), kv->m->caches.end(), kv), kv->m->caches.end());
   }
-  cudaFree(kv->k); cudaFree(kv->v); cudaFree(kv->pos);
-  delete kv;
+  kv_free(kv);
   return SNLP_OK;
 }
 
@@ -1327,6 +1479,13 @@ static Fwd kv_fwd(snlp_model *m, snlp_kv *kv, int T, cudaStream_t st) {
   f.kv_ls = (size_t)kv->B * f.kv_bs;
   f.kv_rows = kv->max_ctx;
   f.pos = kv->pos; f.pos_hi = kv->len_hi; f.st = st;
+  if (kv->pool) {   // the call's own rows are staged in the scratch of the cache-less forwards, [layer][B][T][d]
+    f.kv4 = kv;
+    f.kc = m->sk; f.vc = m->sv;
+    f.kv_bs = (size_t)T * m->cfg.d_model;
+    f.kv_ls = (size_t)kv->B * f.kv_bs;
+    f.kv_rows = T;
+  }
   return f;
 }
 
@@ -1404,7 +1563,7 @@ static int decode_step_impl(snlp_model *m, snlp_kv *kv, const int32_t *tok_in, c
   }
   const bool fast = fast_decode_ok(m, kv->B);
   const int chunk_len = attn_csub(kv->B * m->cfg.n_head) * kAttnSub;
-  GraphKey key{kv->B, sol.K, sol.mode, sol.prefix, sol.init, sol.fuse, fast ? kv->len_hi / chunk_len + 1 : 0, resnorm_out, kv};
+  GraphKey key{kv->B, sol.K, sol.mode, sol.prefix, sol.init, sol.fuse, fast && !kv->pool ? kv->len_hi / chunk_len + 1 : 0, resnorm_out, kv};
   auto it = m->graphs.find(key);
   if (it == m->graphs.end()) {
     if (m->graphs.size() >= 256) {

@@ -60,6 +60,7 @@ struct UmmaParams {
   __nv_bfloat16 *q; size_t q_ls;             // UEPI_QKV
   __nv_bfloat16 *kc, *vc; size_t kv_ls, kv_bs;
   int T, d; const int *pos_base; const float2 *rope; float qk_eps;
+  int kv_local;            // UEPI_QKV: keys / values go to row 0 .. T-1 of the store (a staging area) instead of to their position
   const float2 *rope_t; int rope_ld;  // rope transposed [hd/2][rope_ld], read by the prefill-regime epilogue (thread = row)
   const float *xm; size_t xm_ls; const HcCoef *coef; float *ssq_out;   // UEPI_RESID; ssq_out [nl][partials][M]
   float *logits; float *pm_val; int *pm_idx;                            // UEPI_LMHEAD
@@ -339,14 +340,14 @@ __device__ __forceinline__ void umma_epilogue_rows(const UmmaParams &p, uint32_t
       if (c4 == 0 && grow < p.M) p.ssq_out[(((size_t)l * p.Nt + n_tile) * 2 + grp) * p.M + grow] = v;
     }
   } else if (EPI == UEPI_QKV) {
-    const int Tn = p.T, b = live ? row / Tn : 0, pos = *p.pos_base + (live ? row % Tn : 0);
+    const int Tn = p.T, b = live ? row / Tn : 0, t_row = live ? row % Tn : 0, pos = *p.pos_base + t_row, kv_row = p.kv_local ? t_row : pos;
 #pragma unroll 1
     for (int hh = grp; hh < BN / 128; hh += 2) {   // a 256-wide tile holds two heads, one per warp group
       const int n = n_tile * BN + hh * 128, kind = n / p.d, hcol = n % p.d;
       const uint32_t tcol = tbase + hh * 128;
       __nv_bfloat16 *dst;
       if (kind == 0) dst = p.q + (size_t)l * p.q_ls + (size_t)row * p.d + hcol;
-      else dst = (kind == 1 ? p.kc : p.vc) + (size_t)l * p.kv_ls + (size_t)b * p.kv_bs + (size_t)pos * p.d + hcol;
+      else dst = (kind == 1 ? p.kc : p.vc) + (size_t)l * p.kv_ls + (size_t)b * p.kv_bs + (size_t)kv_row * p.d + hcol;
       if (kind == 2) {
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
@@ -494,7 +495,7 @@ __device__ __forceinline__ void umma_epilogue_small(const UmmaParams &p, const f
         if (lane == 0) p.ssq_out[((size_t)l * p.Nt * (BN / 128) + n_tile * (BN / 128) + h) * p.M + tok] = ss;
       }
     } else if (EPI == UEPI_QKV) {
-      const int b = tok / p.T, pos = q.pos[tt];
+      const int b = tok / p.T, kv_row = p.kv_local ? tok % p.T : q.pos[tt];
       // (the rotation-table entries of this position serve every head of the tile and were fetched before anything is
       // stored: a load that follows a store is not issued ahead of it)
       const float2 c0 = q.c0[tt], c1 = q.c1[tt];
@@ -504,7 +505,7 @@ __device__ __forceinline__ void umma_epilogue_small(const UmmaParams &p, const f
         const float *yh = y + hh * 128;
         __nv_bfloat16 *dst;
         if (kind == 0) dst = p.q + (size_t)l * p.q_ls + (size_t)tok * p.d + hcol;
-        else dst = (kind == 1 ? p.kc : p.vc) + (size_t)l * p.kv_ls + (size_t)b * p.kv_bs + (size_t)pos * p.d + hcol;
+        else dst = (kind == 1 ? p.kc : p.vc) + (size_t)l * p.kv_ls + (size_t)b * p.kv_bs + (size_t)kv_row * p.d + hcol;
         if (kind == 2) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) dst[lane + 32 * j] = __float2bfloat16_rn(yh[lane + 32 * j] * rstd);

@@ -27,7 +27,7 @@ EXPORTS = [
     "snlp_kv_truncate", "snlp_prefill", "snlp_decode_step", "snlp_decode_step_host", "snlp_draft_and_verify", "snlp_set_flag",
     "snlp_launch_count", "snlp_kernel_times", "snlp_device_status", "snlp_lm_head_greedy_static", "snlp_last_error",
     "snlp_copy_trace", "snlp_draft_and_verify_async", "snlp_graph_count",
-    "snlp_kv4_pool_bytes", "snlp_page_plan", "snlp_kv4_write", "snlp_kv4_read", "snlp_kv4_attention_workspace", "snlp_kv4_attention",
+    "snlp_kv_create_4bit", "snlp_kv4_pool_bytes", "snlp_page_plan", "snlp_kv4_write", "snlp_kv4_read", "snlp_kv4_attention_workspace", "snlp_kv4_attention",
 ]
 
 
@@ -105,12 +105,17 @@ def _bf16_bits(x: np.ndarray) -> np.ndarray:
 
 
 class KVCache:
-    def __init__(self, model: "Model", B: int, max_ctx: int):
+    """bits: None = the model's dtype, 4 = codes of 4 bits with a scale per 64 features (snlp_kv_create_4bit)."""
+
+    def __init__(self, model: "Model", B: int, max_ctx: int, bits: int | None = None):
         self.model = model
         self.B = B
         self.max_ctx = max_ctx
         self._h = C.c_void_p()
-        _check(_lib.snlp_kv_create(model._h, C.c_int(B), C.c_int(max_ctx), C.byref(self._h)))
+        if bits not in (None, 4):
+            _refuse(f"a cache holds the model's dtype (bits=None) or 4 bits, not {bits}")
+        create = _lib.snlp_kv_create if bits is None else _lib.snlp_kv_create_4bit
+        _check(create(model._h, C.c_int(B), C.c_int(max_ctx), C.byref(self._h)))
 
     def __len__(self):
         n = C.c_int32()
@@ -215,8 +220,8 @@ class Model:
         return logits, arg
 
     # -- decoding ---------------------------------------------------------------------------------
-    def kv_cache(self, B: int, max_ctx: int) -> KVCache:
-        return KVCache(self, B, max_ctx)
+    def kv_cache(self, B: int, max_ctx: int, bits: int | None = None) -> KVCache:
+        return KVCache(self, B, max_ctx, bits)
 
     def prefill(self, kv: KVCache, ids: torch.Tensor) -> torch.Tensor:
         B, T = ids.shape
