@@ -95,7 +95,7 @@ static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) 
   const Kv4Attn &a = p.a;
   typedef Attn4Smem<HD, NT> S;
   const size_t smem = S::kFixed + (size_t)(a.B + 1) * 4;
-  const int resident = std::min<int>(NT == 1 ? 3 : 2, (int)((size_t)228 * 1024 / (smem + 1024 + 64)));   // 64: the kernel's static arrays
+  const int resident = std::min<int>(kAttn4Resident<T, NT>, (int)((size_t)228 * 1024 / (smem + 1024 + 64)));   // 64: the kernel's static arrays
   // at most this many units; the kernel counts the real ones from the lengths on the device
   const int64_t most = ((int64_t)a.n_rows * p.G / (8 * NT) + a.B) * p.nch_max * a.Hkv * a.nl;
   const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)n_sm * resident));

@@ -9,6 +9,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "kv4.h"
 
@@ -352,14 +354,25 @@ static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_read(Kv4Rows p,
 constexpr int kAttn4Warps = 4, kAttn4Threads = 32 * kAttn4Warps;
 constexpr int kAttn4Stage = 32;   // keys of a stage
 constexpr int kAttn4Ring = 3;     // stages of a warp's ring
+constexpr int kAttn4Batch = 64;   // units whose descriptions are in shared memory at a time
+
+// One unit of the list
+struct Unit4 {
+  int b, h, l;          // sequence, key/value head, layer
+  int r0, nrows;        // first row of the tile within the sequence's T * G rows, rows in it
+  int k0, kend;         // keys of this unit: k0 .. kend-1 (empty: kend <= k0)
+  int c, nch;           // chunk, chunks that the tile's rows can see
+  int tok0, ahead, cap; // first row of the sequence; row i sees keys 0 .. ahead + i, cut to cap keys
+};
 
 template <int HD, int NT>
 struct Attn4Smem {
   static constexpr int kStage = 2 * Kv4Fmt<HD>::kBytes;
   static constexpr int kRing = kAttn4Warps * kAttn4Ring * kStage;
-  static constexpr int kOutLd = HD + 4;                              // outputs, then maximum and denominator
+  static constexpr int kOutLd = HD + 4;                              // outputs, then reference and denominator
   static constexpr int kOut = kAttn4Warps * 8 * NT * kOutLd * 4;
-  static constexpr int kFixed = kRing + kOut;                        // + (B + 1) ints
+  static constexpr int kUnits = kAttn4Batch * (int)sizeof(Unit4);
+  static constexpr int kFixed = kRing + kOut + kUnits;               // + (B + 1) ints
 };
 
 struct Attn4Params {
@@ -371,7 +384,7 @@ struct Attn4Params {
 
 __device__ __forceinline__ float ex2(float x) {
   float r;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));   // results below 2^-126 become 0: nothing beside a largest term of 1
   return r;
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -411,16 +424,7 @@ __device__ __forceinline__ Seq4 seq4(const Kv4Attn &a, int b) {
   s.cap = min(s.len, a.max_len);
   return s;
 }
-__device__ __forceinline__ int seq4_visible(const Seq4 &s, int i) { return min(max(s.len - s.T + i + 1, 0), s.cap); }   // keys that row i sees
-
-// One unit of the list
-struct Unit4 {
-  int b, h, l;          // sequence, key/value head, layer
-  int r0, nrows;        // first row of the tile within the sequence's T * G rows, rows in it
-  int k0, kend;         // keys of this unit: k0 .. kend-1 (empty: kend <= k0)
-  int c, nch;           // chunk, chunks that the tile's rows can see
-  int tok0, T, len, cap;
-};
+__device__ __forceinline__ int seq4_visible(int ahead, int cap, int i) { return min(max(ahead + i + 1, 0), cap); }   // keys that row i sees
 
 template <int NT>
 __device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, int x, int y) {
@@ -433,8 +437,8 @@ __device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, in
   u.c = w % nchb;
   u.r0 = (w / nchb) * (8 * NT);
   u.nrows = min(s.T * p.G - u.r0, 8 * NT);
-  u.tok0 = s.row0; u.T = s.T; u.len = s.len; u.cap = s.cap;
-  const int vis = seq4_visible(s, (u.r0 + u.nrows - 1) / p.G);   // the tile's last row sees most
+  u.tok0 = s.row0; u.ahead = s.len - s.T; u.cap = s.cap;
+  const int vis = seq4_visible(u.ahead, u.cap, (u.r0 + u.nrows - 1) / p.G);   // the tile's last row sees most
   u.nch = max((vis + p.chunk - 1) / p.chunk, 1);
   u.k0 = u.c * p.chunk;
   u.kend = min(u.k0 + p.chunk, vis);
@@ -460,8 +464,12 @@ __device__ __forceinline__ float code_offset(uint32_t par) {
   return CENTRED ? fmaf(8.f, __uint_as_float(par << 16), m) : m;
 }
 
+// blocks of an SM: three fit the shared memory; what needs more than 168 registers runs two
+template <typename T, int NT>
+constexpr int kAttn4Resident = NT == 1 && sizeof(T) == 2 ? 3 : 2;
+
 template <typename T, int HD, int NT>
-static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_attn(const __grid_constant__ Attn4Params p) {
+static __global__ void __launch_bounds__(kAttn4Threads, (kAttn4Resident<T, NT>)) k_kv4_attn(const __grid_constant__ Attn4Params p) {
   typedef Kv4Fmt<HD> F;
   typedef Attn4Smem<HD, NT> S;
   constexpr int NG = F::NG, KS = 4;                       // matrix steps of 16 features per group
@@ -473,6 +481,7 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   unsigned char *ring = attn4_sm + warp * kAttn4Ring * S::kStage;
   float *om = reinterpret_cast<float *>(attn4_sm + S::kRing);
+  Unit4 *units = reinterpret_cast<Unit4 *>(attn4_sm + S::kRing + S::kOut);
   int *uoff = reinterpret_cast<int *>(attn4_sm + S::kFixed);
   const Kv4Attn &a = p.a;
   pdl_wait();
@@ -513,32 +522,39 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
   const long long u0 = total * blockIdx.x / gridDim.x, u1 = total * (blockIdx.x + 1) / gridDim.x;
   if (u0 >= u1) return;
 
-  // ---- copy side: this warp's stages in order, kAttn4Ring - 1 of them ahead of the arithmetic ----
   const int bpp = a.page / kKv4Block, page_sh = 31 - __clz(a.page);
   const size_t page_bytes = (size_t)a.Hkv * bpp * F::kBytes;
-  long long pu = u0;                       // unit
-  int px = (int)(u0 % U), py = (int)(u0 / U), pi = 0, pn = 0, pk0 = 0, pkend = 0;
-  int ent = -1, slot_w = 0;
+  int q_b = -1, q_y = -1, q_r0 = -1;       // whose query rows the fragments hold
+  uint32_t qf[NT][NSP][NG * KS][2];
+  float qfac[NT][2], qsum[NT][2][NG];      // of this thread's two columns: power-of-two factor with the scale, scaled feature sums
+
+  for (long long first = u0; first < u1; first += kAttn4Batch) {
+  const int nu = (int)min(u1 - first, (long long)kAttn4Batch);
+  if (first != u0) __syncthreads();        // every warp is done with the batch before
+  if (tid < nu) units[tid] = unit4<NT>(p, uoff, (int)((first + tid) % U), (int)((first + tid) / U));
+  __syncthreads();
+
+  // ---- copy side: this warp's stages in order, kAttn4Ring - 1 of them ahead of the arithmetic ----
+  int pu = 0, pi = 0, pn = 0, pk0 = 0, ent = -1, slot_w = 0;
   const uint8_t *pbase = nullptr;          // the unit's layer and head within page 0
   auto enter = [&]() {                     // stages of unit pu, and the page of each of their 16-key blocks (lane 2 i + j: block j of stage i)
-    const Unit4 u = unit4<NT>(p, uoff, px, py);
-    pk0 = u.k0; pkend = u.kend; pi = 0;
-    const int ns = (max(pkend - pk0, 0) + kAttn4Stage - 1) / kAttn4Stage;
+    const Unit4 &u = units[pu];
+    const int kend = u.kend;
+    pk0 = u.k0; pi = 0;
+    const int ns = (max(kend - pk0, 0) + kAttn4Stage - 1) / kAttn4Stage;
     pn = (ns - warp + kAttn4Warps - 1) / kAttn4Warps;
     pbase = a.pool + (size_t)u.l * a.pool_ls + (size_t)u.h * bpp * F::kBytes;
     ent = -1;
     const int key = pk0 + ((lane >> 1) * kAttn4Warps + warp) * kAttn4Stage + (lane & 1) * kKv4Block;
-    if ((lane >> 1) < pn && key < pkend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
+    if ((lane >> 1) < pn && key < kend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
   };
   enter();
   auto copy_next = [&]() {                 // request the next stage (if any); always closes a group
-    while (pi >= pn && pu < u1) {
-      ++pu;
-      if (++px == U) { px = 0; ++py; }
-      if (pu < u1) enter();
-    }
-    if (pu < u1) {
-      unsigned char *dst = ring + slot_w * S::kStage;
+    while (pi >= pn && pu < nu)
+      if (++pu < nu) enter();
+    if (pu < nu) {
+      constexpr int NC = F::kBytes / 16;   // 16-byte pieces of a block; piece c = lane + 32 i of the stage
+      unsigned char *dst = ring + slot_w * S::kStage + lane * 16;
       const int key = pk0 + (pi * kAttn4Warps + warp) * kAttn4Stage;
       const uint8_t *src[2];
       bool ok[2];
@@ -546,13 +562,12 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
       for (int j = 0; j < 2; ++j) {
         const int e = __shfl_sync(0xffffffffu, ent, 2 * pi + j);
         ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
-        src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + (size_t)(((key + 16 * j) & (a.page - 1)) / kKv4Block) * F::kBytes;
+        src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + ((key + 16 * j) & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16 - j * F::kBytes;
       }
-      constexpr int NC = F::kBytes / 16;             // 16-byte pieces of a block
 #pragma unroll
       for (int i = 0; i < (2 * NC + 31) / 32; ++i) {
-        const int c = lane + 32 * i, j = c >= NC;
-        if (2 * NC % 32 == 0 || c < 2 * NC) cp_async16(dst + c * 16, (j ? src[1] : src[0]) + (c - j * NC) * 16, j ? ok[1] : ok[0]);
+        const bool j = 32 * i >= NC ? true : 32 * i + 31 < NC ? false : lane >= NC - 32 * i;
+        if (32 * i + 31 < 2 * NC || lane < 2 * NC - 32 * i) cp_async16(dst + 512 * i, (j ? src[1] : src[0]) + 512 * i, j ? ok[1] : ok[0]);
       }
       ++pi;
       slot_w = slot_w + 1 == kAttn4Ring ? 0 : slot_w + 1;
@@ -563,14 +578,11 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
   for (int i = 0; i < kAttn4Ring - 1; ++i) copy_next();
 
   // ---- arithmetic ----
-  int slot_r = 0, cx = (int)(u0 % U), cy = (int)(u0 / U);
-  int q_b = -1, q_y = -1, q_r0 = -1;       // whose query rows the fragments hold
-  uint32_t qf[NT][NSP][NG * KS][2];
-  float qfac[NT][2], qsum[NT][2][NG];      // of this thread's two columns: power-of-two factor with the scale, scaled feature sums
-  for (long long cu = u0; cu < u1; ++cu) {
-    const Unit4 u = unit4<NT>(p, uoff, cx, cy);
-    if (u.b != q_b || cy != q_y || u.r0 != q_r0) {
-      q_b = u.b; q_y = cy; q_r0 = u.r0;
+  int slot_r = 0;
+  for (int cu = 0; cu < nu; ++cu) {
+    const Unit4 u = units[cu];
+    if (u.b != q_b || u.l * a.Hkv + u.h != q_y || u.r0 != q_r0) {
+      q_b = u.b; q_y = u.l * a.Hkv + u.h; q_r0 = u.r0;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int r = nt * 8 + g;          // fragment column g: row r of the tile
@@ -643,16 +655,15 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
         }
       }
     }
-    int vis[NT][2], vis_min = u.cap;       // keys each of this thread's columns sees
-    const Seq4 sq{u.tok0, u.T, u.len, u.cap};
+    int vis[NT][2];                        // keys each of this thread's columns sees
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int col = 0; col < 2; ++col) vis[nt][col] = seq4_visible(sq, (u.r0 + min(nt * 8 + 2 * t + col, u.nrows - 1)) / p.G);
-    vis_min = seq4_visible(sq, u.r0 / p.G);
+      for (int col = 0; col < 2; ++col) vis[nt][col] = seq4_visible(u.ahead, u.cap, (u.r0 + min(nt * 8 + 2 * t + col, u.nrows - 1)) / p.G);
+    const int vis_min = seq4_visible(u.ahead, u.cap, u.r0 / p.G);
 
     float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
-    int E[NG];                              // exponent of the largest value scale so far
+    float lim[NG], pf[NG];                  // E = exponent of the largest value scale so far: 2^(E + 1), 2^(14 - E)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -665,7 +676,7 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
       for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
     }
 #pragma unroll
-    for (int n = 0; n < NG; ++n) E[n] = -100;
+    for (int n = 0; n < NG; ++n) { lim[n] = pow2(-99); pf[n] = pow2(114); }
 
     const int ns = (max(u.kend - u.k0, 0) + kAttn4Stage - 1) / kAttn4Stage;
     for (int si = warp; si < ns; si += kAttn4Warps) {
@@ -675,8 +686,11 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
       copy_next();     // ... whose place is filled again
       const unsigned char *stage = ring + slot_r * S::kStage;
       slot_r = slot_r + 1 == kAttn4Ring ? 0 : slot_r + 1;
-      const bool edge = key0 + kAttn4Stage > vis_min;   // some row does not see all of the stage
       const int ka = (g & 1) * 4 + (g >> 1);            // kappa(g): this thread's score rows are keys ka and ka + 8 of a block
+      // EDGE: some row does not see all of the stage.  A key that a row does not see may hold a NaN (a later token, or whatever
+      // the page held before): it is kept out of the sums by selection, not by a weight of zero.
+      auto stage_body = [&](auto edge_c) {
+      constexpr bool EDGE = decltype(edge_c)::value;
 
       // scores of 2 x 16 keys
       float sc[NT][2][4];
@@ -732,12 +746,12 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
                 off = fmaf(code_offset<CEN>(par), qsum[nt][col][n], off);
               }
               float s = fmaf(qfac[nt][col], dot, off);
-              if (edge && key0 + 16 * j + ka + 8 * row >= vis[nt][col]) s = -INFINITY;
+              if (EDGE && key0 + 16 * j + ka + 8 * row >= vis[nt][col]) s = -INFINITY;
               sc[nt][j][2 * row + col] = s;
             }
       }
 
-      // value parameters of this thread's four keys; keys that no row of the tile sees count as zeros (whatever the page holds there)
+      // value parameters of this thread's four keys; keys that no row of the tile sees count as zeros
       uint32_t vp[2][2][NG];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -750,36 +764,30 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
           } else {
             vp[j][row][0] = *reinterpret_cast<const uint32_t *>(at);
           }
-          if (edge && key0 + 16 * j + ka + 8 * row >= u.kend) {
+          if (EDGE && key0 + 16 * j + ka + 8 * row >= u.kend) {
 #pragma unroll
             for (int n = 0; n < NG; ++n) vp[j][row][n] = 0u;
           }
         }
-      // raise E where a finite scale exceeds it
-      bool up = false;
+      // a scale of 2^(E + 1) or more raises E (fmaxf passes over a NaN)
+      float top[NG], grow[NG];
+      bool rescale = false;
 #pragma unroll
-      for (int n = 0; n < NG; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = (int)((vp[i >> 1][i & 1][n] >> 7) & 0xff) - 127;
-          up = up || (e > E[n] && e != 128);
-        }
-      float grow[NG];
-#pragma unroll
-      for (int n = 0; n < NG; ++n) grow[n] = 1.f;
-      bool rescale = __any_sync(0xffffffffu, up);
+      for (int n = 0; n < NG; ++n) {
+        top[n] = fmaxf(fmaxf(__uint_as_float(vp[0][0][n] << 16), __uint_as_float(vp[0][1][n] << 16)),
+                       fmaxf(__uint_as_float(vp[1][0][n] << 16), __uint_as_float(vp[1][1][n] << 16)));
+        rescale = rescale || top[n] >= lim[n];
+        grow[n] = 1.f;
+      }
+      rescale = __any_sync(0xffffffffu, rescale);
       if (rescale) {
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
-          int e = E[n];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int x = (int)((vp[i >> 1][i & 1][n] >> 7) & 0xff) - 127;
-            if (x != 128) e = max(e, x);
-          }
-          e = __reduce_max_sync(0xffffffffu, e);
-          grow[n] = pow2(max(E[n] - e, -126));
-          E[n] = e;
+          const int was = (int)(__float_as_uint(lim[n]) >> 23) - 128;
+          const int e = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top[n], 0.f))) >> 23) - 127, was), 126);
+          grow[n] = pow2(max(was - e, -126));
+          lim[n] = pow2(e + 1);
+          pf[n] = pow2(14 - e);
         }
       }
 
@@ -810,8 +818,8 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
               sum += pr;
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
-                const float add = pr * code_offset<CEN>(vp[j][row][n]);
-                lo[n] += edge && key0 + 16 * j + ka + 8 * row >= vis[nt][col] ? 0.f : add;   // a key that this row does not see may hold a NaN
+                const float off = code_offset<CEN>(vp[j][row][n]);
+                if (!EDGE || key0 + 16 * j + ka + 8 * row < vis[nt][col]) lo[n] = fmaf(pr, off, lo[n]);
               }
             }
           den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
@@ -848,16 +856,15 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
         uint32_t b[2][NT][NSP][2];
-        const float f = pow2(14 - E[n]);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int row = 0; row < 2; ++row) {
-            const float s = __uint_as_float(vp[j][row][n] << 16) * f;
+            const float s = __uint_as_float(vp[j][row][n] << 16) * pf[n];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float x0 = sc[nt][j][2 * row] * s, x1 = sc[nt][j][2 * row + 1] * s;
-              if (edge) {   // as above: no NaN from a key that the row does not see
+              if (EDGE) {
                 const int key = key0 + 16 * j + ka + 8 * row;
                 x0 = key >= vis[nt][0] ? 0.f : x0;
                 x1 = key >= vis[nt][1] ? 0.f : x1;
@@ -900,10 +907,13 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
             }
           }
       }
+      };
+      if (key0 + kAttn4Stage > vis_min) stage_body(std::true_type{});
+      else stage_body(std::false_type{});
     }
 
     // ---- join the four warps ----
-    if (cu != u0) __syncthreads();   // the previous unit's results have been read
+    if (cu != 0) __syncthreads();   // the previous unit's results have been read
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -923,7 +933,7 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
             // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes)
-            const float back = pow2(E[n] - 14);
+            const float back = lim[n] * pow2(-15);   // 2^(E - 14)
             float y[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -962,9 +972,9 @@ static __global__ void __launch_bounds__(kAttn4Threads, NT == 1 ? 3 : 2) k_kv4_a
         }
       }
     }
-    if (++cx == U) { cx = 0; ++cy; }
   }
   cp_async_wait<0>();
+  }
 }
 
 // Joins the chunks of a row in chunk order: four warps take every fourth chunk each, then the warps in order.
@@ -988,8 +998,8 @@ static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant_
   const int i = tok - s.row0;
   if (i < 0 || i >= s.T) return;
   const int ri = i * p.G + hq % p.G, last = min((ri / tile + 1) * tile, s.T * p.G) - 1;
-  if (seq4_visible(s, last / p.G) <= p.chunk) return;            // the tile had one chunk: its rows are done
-  const int nch = (seq4_visible(s, i) + p.chunk - 1) / p.chunk;
+  if (seq4_visible(s.len - s.T, s.cap, last / p.G) <= p.chunk) return;            // the tile had one chunk: its rows are done
+  const int nch = (seq4_visible(s.len - s.T, s.cap, i) + p.chunk - 1) / p.chunk;
   const size_t row = (size_t)tok * a.Hq + hq;
   const float *src = a.part + ((size_t)l * a.n_rows * a.Hq + row) * p.nch_max * (HD + 4);
   float o[V] = {}, M = -INFINITY, den = 0.f;
