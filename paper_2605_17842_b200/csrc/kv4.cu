@@ -26,15 +26,22 @@ static bool rows_vec(const Kv4Rows &p) {
   return ok(p.k, p.k_ls, p.k_ts, p.k_hs) && ok(p.v, p.v_ls, p.v_ts, p.v_hs);
 }
 
+static int log2_of(int page) { return 31 - __builtin_clz((unsigned)page); }
+
 template <bool WRITE>
 static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
   if (p.n < 1) return cudaSuccess;
-  const dim3 grid((unsigned)((p.n + kKv4Block - 1) / kKv4Block) * p.H, p.nl);
+  // heads of a block: one while there are few blocks (a decode step's tokens: latency counts), several when there are many, so
+  // that the slot is looked up once and the next head's loads follow
+  const int64_t tg = ((int64_t)p.n + kKv4Block - 1) / kKv4Block;
+  const int hpb = tg * p.H * p.nl < 4096 ? 1 : 4;
+  const dim3 grid((unsigned)(tg * ((p.H + hpb - 1) / hpb)), p.nl);
   const bool vec = rows_vec(p);
-#define KV4_ROWS(T, HD)                                                       \
-  do {                                                                        \
-    if (WRITE) k_kv4_write<T, HD><<<grid, kRowsThreads(HD), 0, st>>>(p, vec); \
-    else k_kv4_read<T, HD><<<grid, kRowsThreads(HD), 0, st>>>(p, vec);        \
+  const int sh = log2_of(p.page);
+#define KV4_ROWS(T, HD)                                                                 \
+  do {                                                                                  \
+    if (WRITE) k_kv4_write<T, HD><<<grid, kWriteThreads(HD), 0, st>>>(p, vec, hpb, sh); \
+    else k_kv4_read<T, HD><<<grid, kReadThreads, 0, st>>>(p, vec, hpb, sh);             \
   } while (0)
   if (p.fp32) {
     if (p.hd == 128) KV4_ROWS(float, 128); else KV4_ROWS(float, 64);
@@ -63,14 +70,16 @@ size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, in
   return n < 2 ? 0 : (size_t)nl * n_rows * Hq * n * (hd + 4) * sizeof(float);
 }
 
-template <typename T, int HD, int NT>
-static cudaError_t attn_attr() {
-  return cudaFuncSetAttribute(k_kv4_attn<T, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn4Smem<HD, NT>::kFixed + (kKv4MaxBatch + 1) * 4);
+template <typename T, int HD, int RW, int NT>
+static cudaError_t attn_attr1() {
+  return cudaFuncSetAttribute(k_kv4_attn<T, HD, RW, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn4Cfg<T, HD, RW, NT>::kFixed + (kKv4MaxBatch + 1) * 4);
 }
 template <typename T, int HD>
-static cudaError_t attn_attr2() {
-  const cudaError_t e = attn_attr<T, HD, 1>();
-  return e != cudaSuccess ? e : attn_attr<T, HD, 2>();
+static cudaError_t attn_attr() {
+  cudaError_t e = attn_attr1<T, HD, 2, 1>();
+  if (e == cudaSuccess) e = attn_attr1<T, HD, 4, 1>();
+  if (e == cudaSuccess) e = attn_attr1<T, HD, 8, 1>();
+  return e != cudaSuccess ? e : attn_attr1<T, HD, 8, 2>();
 }
 
 cudaError_t kv4_init() {
@@ -81,25 +90,25 @@ cudaError_t kv4_init() {
   if (e != cudaSuccess) return e;
   std::lock_guard<std::mutex> lock(mu);
   if (dev < 64 && done[dev]) return cudaSuccess;
-  e = attn_attr2<float, 64>();
-  if (e == cudaSuccess) e = attn_attr2<float, 128>();
-  if (e == cudaSuccess) e = attn_attr2<__nv_bfloat16, 64>();
-  if (e == cudaSuccess) e = attn_attr2<__nv_bfloat16, 128>();
+  e = attn_attr<float, 64>();
+  if (e == cudaSuccess) e = attn_attr<float, 128>();
+  if (e == cudaSuccess) e = attn_attr<__nv_bfloat16, 64>();
+  if (e == cudaSuccess) e = attn_attr<__nv_bfloat16, 128>();
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv4_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (kKv4MaxBatch + 1) * 4);
   if (e == cudaSuccess && dev < 64) done[dev] = true;
   return e;
 }
 
-template <typename T, int HD, int NT>
+template <typename T, int HD, int RW, int NT>
 static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) {
   const Kv4Attn &a = p.a;
-  typedef Attn4Smem<HD, NT> S;
+  typedef Attn4Cfg<T, HD, RW, NT> S;
   const size_t smem = S::kFixed + (size_t)(a.B + 1) * 4;
-  const int resident = std::min<int>(kAttn4Resident<T, NT>, (int)((size_t)228 * 1024 / (smem + 1024 + 64)));   // 64: the kernel's static arrays
+  const int resident = std::min<int>(S::kResident, (int)((size_t)228 * 1024 / (smem + 1024 + 64)));   // 64: the kernel's static arrays
   // at most this many units; the kernel counts the real ones from the lengths on the device
-  const int64_t most = ((int64_t)a.n_rows * p.G / (8 * NT) + a.B) * p.nch_max * a.Hkv * a.nl;
+  const int64_t most = ((int64_t)a.n_rows * p.G / (RW * NT) + a.B) * p.nch_max * a.Hkv * a.nl;
   const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)n_sm * resident));
-  k_kv4_attn<T, HD, NT><<<grid, kAttn4Threads, smem, st>>>(p);
+  k_kv4_attn<T, HD, RW, NT><<<grid, kAttn4Threads, smem, st>>>(p);
   if (p.nch_max > 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.n_rows * a.Hq, a.nl); cfg.blockDim = dim3(128); cfg.stream = st;
@@ -107,9 +116,19 @@ static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) 
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // scheduled while the splits finish, waits for their results
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, k_kv4_merge<T, HD>, p, 8 * NT);
+    cudaLaunchKernelEx(&cfg, k_kv4_merge<T, HD>, p, RW * NT);
   }
   return cudaGetLastError();
+}
+
+template <typename T, int HD>
+static cudaError_t attn_pick(const Attn4Params &p, int tile, int n_sm, cudaStream_t st) {
+  switch (tile) {
+    case 2: return attn_launch<T, HD, 2, 1>(p, n_sm, st);
+    case 4: return attn_launch<T, HD, 4, 1>(p, n_sm, st);
+    case 8: return attn_launch<T, HD, 8, 1>(p, n_sm, st);
+    default: return attn_launch<T, HD, 8, 2>(p, n_sm, st);
+  }
 }
 
 cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
@@ -121,13 +140,11 @@ cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
   p.qk_scale = a.scale * 1.4426950408889634f;
   const size_t u = a.fp32 ? 4 : 8;
   p.vec = (uintptr_t)a.q % 16 == 0 && a.q_ls % u == 0 && a.q_ts % u == 0 && a.q_hs % u == 0;
-  // one tile of 8 query rows a unit where a sequence brings no more (decoding), two beyond: the codes are unpacked once for
-  // 16 rows instead of 8
-  const bool two = (int64_t)a.n_rows * p.G > (int64_t)8 * a.B;
-#define KV4_ATTN(T, HD) (two ? attn_launch<T, HD, 2>(p, n_sm, st) : attn_launch<T, HD, 1>(p, n_sm, st))
-  if (a.fp32) return a.hd == 128 ? KV4_ATTN(float, 128) : KV4_ATTN(float, 64);
-  return a.hd == 128 ? KV4_ATTN(__nv_bfloat16, 128) : KV4_ATTN(__nv_bfloat16, 64);
-#undef KV4_ATTN
+  // rows that a sequence brings to a key/value head, on average: the smallest tile that holds them
+  const int64_t rows = ((int64_t)a.n_rows * p.G + a.B - 1) / a.B;
+  const int tile = a.tile ? a.tile : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  if (a.fp32) return a.hd == 128 ? attn_pick<float, 128>(p, tile, n_sm, st) : attn_pick<float, 64>(p, tile, n_sm, st);
+  return a.hd == 128 ? attn_pick<__nv_bfloat16, 128>(p, tile, n_sm, st) : attn_pick<__nv_bfloat16, 64>(p, tile, n_sm, st);
 }
 
 }  // namespace snlp
@@ -237,6 +254,8 @@ static int attn_check(const snlp_kv4_attn *a, const snlp_kv4_pool *pool, const c
   if (a->B > kKv4MaxBatch) return refuse(SNLP_ERR_SHAPE, "%s: B = %d exceeds %d", who, a->B, kKv4MaxBatch);
   if (a->n_head % pool->n_kv_head) return refuse(SNLP_ERR_ARG, "%s: n_head = %d is not a multiple of n_kv_head = %d", who, a->n_head, pool->n_kv_head);
   if (!a->cu_q && a->n_rows % a->B) return refuse(SNLP_ERR_ARG, "%s: without cu_q every sequence has n_rows / B rows: %d is not a multiple of %d", who, a->n_rows, a->B);
+  if (a->tile_rows != 0 && a->tile_rows != 2 && a->tile_rows != 4 && a->tile_rows != 8 && a->tile_rows != 16)
+    return refuse(SNLP_ERR_ARG, "%s: tile_rows must be 0, 2, 4, 8 or 16 (got %d)", who, a->tile_rows);
   if (a->max_len < 0) return refuse(SNLP_ERR_ARG, "%s: max_len must be >= 0", who);
   const int64_t cap = (int64_t)a->max_pages * pool->page_size;
   if (cap > 0x7fffffffLL - 2048) return refuse(SNLP_ERR_SHAPE, "%s: max_pages * page_size exceeds the positions of a sequence", who);
@@ -276,7 +295,7 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   if (need > 0 && (!workspace || workspace_bytes < need)) return refuse(SNLP_ERR_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : (size_t)0, need);
   if ((uintptr_t)workspace % 16) return refuse(SNLP_ERR_ARG, "%s: the workspace must be 16-byte aligned", who);
   const int64_t G = args->n_head / pool->n_kv_head;
-  const int64_t units = (args->n_rows * G / 8 + args->B) * (int64_t)(((int64_t)a.max_len + 255) / 256);
+  const int64_t units = (args->n_rows * G / 2 + args->B) * (int64_t)(((int64_t)a.max_len + 255) / 256);
   if (units > 0x7fffffffLL || (int64_t)args->n_rows * args->n_head > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
   if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
   int dev = 0, n_sm = 0;
@@ -287,7 +306,7 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   a.pool = (const uint8_t *)pool->pages; a.table = args->block_table; a.tstride = args->max_pages; a.lens = args->lens; a.cu = args->cu_q;
   a.out = out; a.part = (float *)workspace;
   a.T = args->n_rows / args->B; a.n_rows = args->n_rows; a.B = args->B; a.Hq = args->n_head; a.Hkv = pool->n_kv_head; a.hd = pool->head_dim;
-  a.n_pages = pool->n_pages; a.page = pool->page_size; a.nl = 1; a.fp32 = args->dtype == SNLP_DTYPE_FP32;
+  a.n_pages = pool->n_pages; a.page = pool->page_size; a.nl = 1; a.tile = args->tile_rows; a.fp32 = args->dtype == SNLP_DTYPE_FP32;
   a.scale = args->scale != 0.f ? args->scale : (pool->head_dim == 128 ? 0.08838834764831845f : 0.125f);
   return launched(kv4_attention(a, n_sm, (cudaStream_t)stream), who);
 }

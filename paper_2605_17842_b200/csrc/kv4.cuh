@@ -147,9 +147,10 @@ static __global__ void __launch_bounds__(kPlanThreads) k_kv4_plan(Kv4Plan p) {
 // Write.  Per (token, head, group): lo = min x, hi = max x; s = bf16(fp32((hi - lo) / 15)), m = bf16(lo);
 // c = round-half-even((x - m) / s) in 0..15 (0 where s = 0).  A group that holds a NaN or an infinity, or whose s or m leaves
 // bf16's range, is stored with s = m = NaN: what reads it sees NaN instead of a silently wrong number.
-// A thread holds 8 features (one word of codes) of a key row and of the same value row; 8 threads share a group.  A block
-// covers 16 consecutive tokens of one head, so the rows of a storage block are written together.  Bound by HBM: each input
-// is read once and each code written once.
+// A thread holds 16 features of a key row and the same of the value row; 4 threads share a group, so the reductions take two
+// exchanges and a division serves 16 elements.  Rounding and packing run on the multiply-add pipe: x / s + 1.5 * 2^23 has
+// the code in its low bits, and eight of them are added up shifted.  A block covers 16 consecutive tokens of one or more
+// heads, so the rows of a storage block are written together.  Bound by HBM and instruction issue about equally.
 __device__ __forceinline__ float min_nan(float a, float b) {   // NaN if either is (fminf would drop it)
   float r;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -222,79 +223,125 @@ __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, bool vec
   }
 }
 
-// Codes of 8 features of a group whose 64 lie in 8 consecutive lanes (all 32 lanes call).  par = (s, m) as bf16 bits.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &par) {
-  float lo = x[0], hi = x[0];
+// Codes of 16 features of a group whose 64 lie in 4 consecutive lanes (all 32 lanes call).  src: where x came from.
+// par = (s, m) as bf16 bits.
+template <typename T>
+__device__ __forceinline__ void quantise16(const float (&x)[2][8], const T *src, uint32_t (&word)[2], uint32_t &par) {
+  float lo = x[0][0], hi = x[0][0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
+  for (int i = 1; i < 16; ++i) { lo = min_nan(lo, x[i >> 3][i & 7]); hi = max_nan(hi, x[i >> 3][i & 7]); }
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) {
+  for (int o = 1; o < 4; o <<= 1) {
     lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
   const float r = __fsub_rn(hi, lo);
   // r / 15 in fp32 is the rounding of the true quotient wherever hi - lo has no error of its own; else through fp64
-  const float quo = diff_err(hi, lo, r) == 0.f ? __fdiv_rn(r, 15.f) : (float)(((double)hi - (double)lo) / 15.0);
+  float quo = __fdiv_rn(r, 15.f);
+  if (diff_err(hi, lo, r) != 0.f) quo = (float)(((double)hi - (double)lo) / 15.0);
   const float s = __bfloat162float(__float2bfloat16_rn(quo)), m = __bfloat162float(__float2bfloat16_rn(lo));
+  word[0] = word[1] = 0u;
   if (!(isfinite(s) && isfinite(m))) {
     par = 0x7fc07fc0u;
-    return 0u;
+    return;
   }
   par = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
-  if (s == 0.f) return 0u;
-  const float half = 0.5f * s, inv = __fdiv_rn(1.f, s);
-  const bool tiny = s < 1e-30f;   // 1/s may overflow
-  uint32_t word = 0u;
+  if (s == 0.f) return;
+  constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: its unit is 1
+  const bool tiny = s < 1e-30f;          // 1/s may overflow
+  const float half = 0.5f * s, inv = tiny ? 0.f : __fdividef(1.f, s);
+  uint32_t check = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float a = __fsub_rn(x[i], m);
-    float c = rintf(tiny ? __fdiv_rn(a, s) : a * inv);
-    // a * inv may be off by a few units in the last place: where that could have crossed the border between two codes, the
-    // exact remainder (a - c s has no rounding error here) and the error of a decide; a tie goes to the even code
-    const float d = fmaf(-c, s, a);
-    if (fabsf(d) >= half) {
-      const float e = diff_err(x[i], m, a);
-      const bool odd = ((int)c & 1) != 0;
-      if (d > half || (d == half && (e > 0.f || (e == 0.f && odd)))) c += 1.f;
-      else if (d < -half || (d == -half && (e < 0.f || (e == 0.f && odd)))) c -= 1.f;
-    }
-    c = fminf(fmaxf(c, 0.f), 15.f);
-    word |= (uint32_t)(int)c << (4 * i);
+  for (int i = 0; i < 16; ++i) {
+    const float a = __fsub_rn(x[i >> 3][i & 7], m);
+    float t = fmaf(a, inv, kMagic);
+    const float c = __fsub_rn(t, kMagic);
+    // a * inv may be off by a few units in the last place: codes whose exact remainder (a - c s has no rounding error here) is
+    // not below half a step are looked at again
+    if (!(fabsf(fmaf(-c, s, a)) < half)) check |= 1u << i;
+    t = fminf(fmaxf(t, kMagic), kMagic + 15.f);
+    word[i >> 3] += __float_as_uint(t) << (4 * (i & 7));
   }
-  return word;
+  // the bits of 1.5 * 2^23 that were added up with the codes: 0x4b400000 shifted by 0, 4, .. 28 places
+  constexpr uint32_t kBias = 0x4b400000u + 0xb4000000u + 0x40000000u;
+  word[0] -= kBias;
+  word[1] -= kBias;
+  while (check) {
+    const int i = __ffs(check) - 1;
+    check &= check - 1;
+    const float xi = to_f<T>(src[i]), a = __fsub_rn(xi, m);
+    float c = tiny ? rintf(fminf(fmaxf(__fdiv_rn(a, s), -1.f), 16.f)) : __fsub_rn(fmaf(a, inv, kMagic), kMagic);
+    // the exact remainder and the error of a decide; a tie goes to the even code
+    const float d = fmaf(-c, s, a), e = diff_err(xi, m, a);
+    const bool odd = ((int)c & 1) != 0;
+    if (d > half || (d == half && (e > 0.f || (e == 0.f && odd)))) c += 1.f;
+    else if (d < -half || (d == -half && (e < 0.f || (e == 0.f && odd)))) c -= 1.f;
+    const uint32_t code = (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+    const int at = 4 * (i & 7);
+    if (i < 8) word[0] = (word[0] & ~(15u << at)) | code << at;
+    else word[1] = (word[1] & ~(15u << at)) | code << at;
+  }
 }
 
-constexpr int kRowsThreads(int hd) { return kKv4Block * hd / 8; }   // 16 tokens of one head
+// address of the storage block and place in it of a slot, for head 0 (head h: h * page / 16 blocks further); page = 2^page_sh
+struct Place4 {
+  uint8_t *blk;
+  int t;
+};
+__device__ __forceinline__ Place4 place4(const Kv4Rows &p, int l, long long slot, int page_sh, int block_bytes) {
+  const long long pg = slot >> page_sh;
+  const int off = (int)slot & (p.page - 1);
+  return {p.pool + (size_t)l * p.pool_ls + (((size_t)pg * p.H << (page_sh - 4)) + off / kKv4Block) * block_bytes, off % kKv4Block};
+}
 
+// threads of a block: 16 tokens x the threads of a row
+constexpr int kWriteThreads(int hd) { return kKv4Block * hd / 16; }
+constexpr int kReadThreads = kKv4Block * 8;
+
+// grid (16-token groups x head groups of `hpb` heads, layers)
 template <typename T, int HD>
-static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_write(Kv4Rows p, bool vec) {
+static __global__ void __launch_bounds__(kWriteThreads(HD)) k_kv4_write(Kv4Rows p, bool vec, int hpb, int page_sh) {
   typedef Kv4Fmt<HD> F;
-  constexpr int LPR = HD / 8;
-  const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
-  const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
+  constexpr int LPR = HD / 16;
+  const int j = threadIdx.x % LPR, hg = (p.H + hpb - 1) / hpb, l = blockIdx.y;
+  const int h0 = (int)(blockIdx.x % hg) * hpb, h1 = min(h0 + hpb, p.H);
+  const long long tok = (long long)(blockIdx.x / hg) * kKv4Block + threadIdx.x / LPR;
   const long long slot = tok < p.n ? p.slots[(size_t)l * p.slots_ls + tok] : -1;
   const bool live = slot >= 0 && slot < p.n_slots;
-  float xk[8] = {}, xv[8] = {};
-  if (live) {
-    load8<T>((const T *)p.k + (size_t)l * p.k_ls + (size_t)tok * p.k_ts + (size_t)head * p.k_hs + 8 * j, vec, xk);
-    load8<T>((const T *)p.v + (size_t)l * p.v_ls + (size_t)tok * p.v_ts + (size_t)head * p.v_hs + 8 * j, vec, xv);
-  }
-  uint32_t pk, pv;
-  const uint32_t wk = quantise8(xk, pk), wv = quantise8(xv, pv);
-  if (!live) return;
-  const long long pg = slot / p.page;
-  const int off = (int)(slot - pg * p.page), t = off % kKv4Block;
-  uint8_t *blk = p.pool + (size_t)l * p.pool_ls + (((size_t)pg * p.H + head) * (p.page / kKv4Block) + off / kKv4Block) * F::kBytes;
-  reinterpret_cast<uint32_t *>(blk + F::KC + t * F::kCodes)[F::key_word(j)] = wk;
-  reinterpret_cast<uint32_t *>(blk + F::VC + t * F::kCodes)[F::val_word(j)] = wv;
-  if ((j & 7) == 0) {
-    reinterpret_cast<uint32_t *>(blk + F::KP + t * F::kPar)[j >> 3] = pk;
-    reinterpret_cast<uint32_t *>(blk + F::VP + t * F::kPar)[j >> 3] = pv;
+  const T *k = (const T *)p.k + (live ? (size_t)l * p.k_ls + (size_t)tok * p.k_ts : 0) + 16 * j;
+  const T *v = (const T *)p.v + (live ? (size_t)l * p.v_ls + (size_t)tok * p.v_ts : 0) + 16 * j;
+  const Place4 at = place4(p, l, live ? slot : 0, page_sh, F::kBytes);
+  const size_t head_bytes = (size_t)(p.page / kKv4Block) * F::kBytes;
+  const int grp = j / 4, r = j % 4;   // group of this thread's features, place in it
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    float xk[2][8] = {}, xv[2][8] = {};
+    const T *ks = k + (size_t)h * p.k_hs, *vs = v + (size_t)h * p.v_hs;
+    if (live) {
+      load8<T>(ks, vec, xk[0]); load8<T>(ks + 8, vec, xk[1]);
+      load8<T>(vs, vec, xv[0]); load8<T>(vs + 8, vec, xv[1]);
+    }
+    uint32_t pk, pv, wk[2], wv[2];
+    quantise16<T>(xk, ks, wk, pk);
+    quantise16<T>(xv, vs, wv, pv);
+    if (live) {
+      uint8_t *blk = at.blk + h * head_bytes;
+      // key words 2r, 2r + 1 of a group lie side by side; value words at (2r) NG + grp, (2r + 1) NG + grp
+      *reinterpret_cast<uint2 *>(blk + F::KC + at.t * F::kCodes + 4 * F::key_word(8 * grp + 2 * r)) = make_uint2(wk[0], wk[1]);
+      uint32_t *dv = reinterpret_cast<uint32_t *>(blk + F::VC + at.t * F::kCodes);
+      dv[F::val_word(8 * grp + 2 * r)] = wv[0];
+      dv[F::val_word(8 * grp + 2 * r + 1)] = wv[1];
+      if (r == 0) {
+        reinterpret_cast<uint32_t *>(blk + F::KP + at.t * F::kPar)[grp] = pk;
+        reinterpret_cast<uint32_t *>(blk + F::VP + at.t * F::kPar)[grp] = pv;
+      }
+    }
   }
 }
 
 // Read: value = s * c + m with one rounding (s * c is exact: 8 + 4 bits), then to T.  Rows whose slot is outside the pool
-// come back as zeros.  Bound by the writes of the unpacked rows.
+// come back as zeros.  A thread holds the same word of every group, so that a warp's stores are whole lines; the loads of two
+// heads are in flight at a time.  Bound by HBM, mostly by the writes of the unpacked rows.
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t par, float (&x)[8]) {
   const float s = __uint_as_float(par << 16), m = __uint_as_float(par & 0xffff0000u);
 #pragma unroll
@@ -302,38 +349,70 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t par, float (&x)[8])
 }
 
 template <typename T, int HD>
-static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_read(Kv4Rows p, bool vec) {
+static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, bool vec, int hpb, int page_sh) {
   typedef Kv4Fmt<HD> F;
-  constexpr int LPR = HD / 8;
-  const int j = threadIdx.x % LPR, head = blockIdx.x % p.H, l = blockIdx.y;
-  const long long tok = (long long)(blockIdx.x / p.H) * kKv4Block + threadIdx.x / LPR;
+  constexpr int NG = F::NG, UN = 2;
+  const int j = threadIdx.x % 8, hg = (p.H + hpb - 1) / hpb, l = blockIdx.y;
+  const int h0 = (int)(blockIdx.x % hg) * hpb, h1 = min(h0 + hpb, p.H);
+  const long long tok = (long long)(blockIdx.x / hg) * kKv4Block + threadIdx.x / 8;
   if (tok >= p.n) return;
   const long long slot = p.slots[(size_t)l * p.slots_ls + tok];
-  float xk[8] = {}, xv[8] = {};
-  if (slot >= 0 && slot < p.n_slots) {
-    const long long pg = slot / p.page;
-    const int off = (int)(slot - pg * p.page), t = off % kKv4Block;
-    const uint8_t *blk = p.pool + (size_t)l * p.pool_ls + (((size_t)pg * p.H + head) * (p.page / kKv4Block) + off / kKv4Block) * F::kBytes;
-    const uint32_t wk = __ldg(reinterpret_cast<const uint32_t *>(blk + F::KC + t * F::kCodes) + F::key_word(j));
-    const uint32_t wv = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VC + t * F::kCodes) + F::val_word(j));
-    const uint32_t pk = __ldg(reinterpret_cast<const uint32_t *>(blk + F::KP + t * F::kPar) + (j >> 3));
-    const uint32_t pv = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VP + t * F::kPar) + (j >> 3));
-    unpack8(wk, pk, xk);
-    unpack8(wv, pv, xv);
+  const bool live = slot >= 0 && slot < p.n_slots;
+  T *k = (T *)p.k + (size_t)l * p.k_ls + (size_t)tok * p.k_ts + 8 * j, *v = (T *)p.v + (size_t)l * p.v_ls + (size_t)tok * p.v_ts + 8 * j;
+  const Place4 at = place4(p, l, live ? slot : 0, page_sh, F::kBytes);
+  const size_t head_bytes = (size_t)(p.page / kKv4Block) * F::kBytes;
+#pragma unroll 1
+  for (int hb = h0; hb < h1; hb += UN) {
+    uint32_t wk[UN][NG], wv[UN][NG], pk[UN][NG], pv[UN][NG];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+#pragma unroll
+      for (int n = 0; n < NG; ++n) wk[u][n] = wv[u][n] = pk[u][n] = pv[u][n] = 0u;   // (codes 0, s = m = 0)
+      if (live && hb + u < h1) {
+        const uint8_t *blk = at.blk + (hb + u) * head_bytes;
+        const uint32_t *ck = reinterpret_cast<const uint32_t *>(blk + F::KC + at.t * F::kCodes);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) wk[u][n] = __ldg(ck + F::key_word(8 * n + j));
+        if constexpr (NG == 2) {
+          const uint2 c = __ldg(reinterpret_cast<const uint2 *>(blk + F::VC + at.t * F::kCodes) + j);
+          const uint2 a = __ldg(reinterpret_cast<const uint2 *>(blk + F::KP + at.t * F::kPar)), b = __ldg(reinterpret_cast<const uint2 *>(blk + F::VP + at.t * F::kPar));
+          wv[u][0] = c.x; wv[u][1] = c.y; pk[u][0] = a.x; pk[u][1] = a.y; pv[u][0] = b.x; pv[u][1] = b.y;
+        } else {
+          wv[u][0] = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VC + at.t * F::kCodes) + j);
+          pk[u][0] = __ldg(reinterpret_cast<const uint32_t *>(blk + F::KP + at.t * F::kPar));
+          pv[u][0] = __ldg(reinterpret_cast<const uint32_t *>(blk + F::VP + at.t * F::kPar));
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      if (hb + u >= h1) break;
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        float x[8];
+        unpack8(wk[u][n], pk[u][n], x);
+        store8<T>(k + (size_t)(hb + u) * p.k_hs + n * kKv4Group, vec, x);
+        unpack8(wv[u][n], pv[u][n], x);
+        store8<T>(v + (size_t)(hb + u) * p.v_hs + n * kKv4Group, vec, x);
+      }
+    }
   }
-  store8<T>((T *)p.k + (size_t)l * p.k_ls + (size_t)tok * p.k_ts + (size_t)head * p.k_hs + 8 * j, vec, xk);
-  store8<T>((T *)p.v + (size_t)l * p.v_ls + (size_t)tok * p.v_ts + (size_t)head * p.v_hs + 8 * j, vec, xv);
 }
 
 // ---------------------------------------------------------------------------------------------------
 // Attention.  Row i of sequence b (T_b rows, len_b keys) sees keys 0 .. len_b - T_b + i:
 //   q . k_j = sum_g s_jg (q_g . c_jg) + m_jg (sum q_g),      o_g = sum_j (p_j s_jg) c_jg + sum_j p_j m_jg,   p = softmax.
 // Both products run on the tensor cores (m16n8k16, fp16 operands, fp32 accumulation) with the CODES as the 16-row operand
-// and up to 8 query rows as the 8 columns: the parameters are applied to the scores and to the probabilities, never to the
-// codes, so a code costs 5/8 of an instruction: `word & 0x000f000f` is a pair of codes as fp16 subnormals c 2^-24,
-// `word & 0x00f000f0` a pair c 2^-20 (exact; the powers of two are taken back in fp32).  The order of the 64 features of a
-// group in the sum is free, and so is the order of the 16 keys: the storage order of words and the key permutation
-// (row r of the score tile holds key kappa(r), kappa(2t) = t, kappa(2t+1) = t + 4) make every fragment a plain load.
+// and 8 columns of queries: the parameters are applied to the scores and to the probabilities, never to the codes, so a code
+// costs 5/8 of an instruction: `word & 0x000f000f` is a pair of codes as fp16 subnormals c 2^-24, `word & 0x00f000f0` a pair
+// c 2^-20 (exact; the powers of two are taken back in fp32).  The order of the 64 features of a group in the sum is free, and
+// so is the order of the 16 keys: the storage order of words and the key permutation (row r of the score tile holds key
+// kappa(r), kappa(2t) = t, kappa(2t+1) = t + 4) make every fragment a plain load.
+// Columns.  With RW < 8 query rows the 8 columns would be mostly empty, and every lane would apply parameters and take
+// exponentials for nothing.  So SUB = 8 / RW blocks of 16 keys share one score tile: column c stands for row c % RW and for
+// the keys of every SUB-th block, c / RW.  (The queries are in all columns; of a block's products a lane keeps those of its
+// own columns, and of the probabilities a block sees its own columns' only.)  Each column has its own running maximum,
+// denominator and accumulator, as if it were a split of its own; they are joined at the end of a unit.
 // fp16 operands.  A query row is multiplied by the power of two that brings its largest element to [2^14, 2^15): a bf16 row
 // is then exact in fp16 down to 2^-24 of its maximum.  The probability times its scale is brought below 2^15 by a power of
 // two from the largest scale seen (raised with an exact rescale of the accumulator, as the running maximum is) and rounded
@@ -343,18 +422,16 @@ static __global__ void __launch_bounds__(kRowsThreads(HD)) k_kv4_read(Kv4Rows p,
 // codes enter as c - 8 (fp16 numbers, three instructions a pair; m + 8 s takes the place of m), a query element (and a
 // probability times its scale) is split into a multiple of 16 (11 bits on one grid for the whole row: the products with
 // codes are whole numbers and their sums exact) and an fp16 remainder with an accumulator of its own, 22 bits in all, and
-// the second product's sums over a stage's 32 keys are added to the running output by fp32 additions, which round.
-// Work.  A unit is (layer, key/value head, sequence, tile of 8 NT query rows, chunk of keys); a block of four warps takes
-// a contiguous range of the list of all units (its place in it comes from a prefix sum over the lengths), each warp every
-// fourth 32-key stage of a unit, through its own ring of cp.async stages that runs on across units.  The block joins its
-// warps' results in warp order; rows with several chunks are joined by k_kv4_merge in chunk order.  Chunk boundaries depend
-// on the number of (sequence, head) pairs only and a row's arithmetic on nothing but its own visible keys, so a row comes
-// out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
-// Bound: HBM for few rows (hd 128: 144 bytes a key and head), the mma.sync rate beyond ~16 rows per key/value head.
+// the second product's sums over a block's keys are added to the running output by fp32 additions, which round.
+// Work.  A unit is (layer, key/value head, sequence, tile of RW NT query rows, chunk of keys); a thread block of four warps
+// takes a contiguous range of the list of all units (its place in it comes from a prefix sum over the lengths), each warp
+// every fourth stage of a unit, through its own ring of cp.async stages that runs on across units.  The block joins its
+// warps' columns in a fixed order; rows with several chunks are joined by k_kv4_merge in chunk order.  Chunk boundaries
+// depend on the number of (sequence, head) pairs only and a row's arithmetic on its own visible keys and RW, so for one RW a
+// row comes out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
+// Bound: HBM for few rows (hd 128: 144 bytes a key and head), instruction issue and the mma.sync rate beyond.
 constexpr int kAttn4Warps = 4, kAttn4Threads = 32 * kAttn4Warps;
-constexpr int kAttn4Stage = 32;   // keys of a stage
-constexpr int kAttn4Ring = 3;     // stages of a warp's ring
-constexpr int kAttn4Batch = 64;   // units whose descriptions are in shared memory at a time
+constexpr int kAttn4Batch = 16;   // units whose descriptions are in shared memory at a time
 
 // One unit of the list
 struct Unit4 {
@@ -363,16 +440,27 @@ struct Unit4 {
   int k0, kend;         // keys of this unit: k0 .. kend-1 (empty: kend <= k0)
   int c, nch;           // chunk, chunks that the tile's rows can see
   int tok0, ahead, cap; // first row of the sequence; row i sees keys 0 .. ahead + i, cut to cap keys
+  int vis0, vis1;       // keys that the tile's first and last row see
 };
 
-template <int HD, int NT>
-struct Attn4Smem {
-  static constexpr int kStage = 2 * Kv4Fmt<HD>::kBytes;
-  static constexpr int kRing = kAttn4Warps * kAttn4Ring * kStage;
-  static constexpr int kOutLd = HD + 4;                              // outputs, then reference and denominator
-  static constexpr int kOut = kAttn4Warps * 8 * NT * kOutLd * 4;
-  static constexpr int kUnits = kAttn4Batch * (int)sizeof(Unit4);
-  static constexpr int kFixed = kRing + kOut + kUnits;               // + (B + 1) ints
+template <typename T, int HD, int RW, int NT>
+struct Attn4Cfg {
+  static_assert(NT == 1 || RW == 8, "several column tiles only with full ones");
+  static constexpr int SUB = 8 / RW;            // blocks of keys that share a score tile
+  static constexpr int KB = RW <= 4 ? 4 : 2;    // blocks of a stage
+  static constexpr int NSET = KB / SUB;         // score tiles of a stage (per column tile)
+  static constexpr int kKeys = KB * kKv4Block;  // keys of a stage
+  static constexpr int kRingLen = KB == 4 ? 2 : 3;
+  // blocks of a stage that are read side by side (by the lanes of different columns) start on different banks
+  __host__ __device__ static constexpr int block_at(int j) { return j * Kv4Fmt<HD>::kBytes + (SUB == 1 ? 0 : HD == 128 ? (j & 1) * 16 + (j >> 1) * 64 : j * 32); }
+  static constexpr int kStage = block_at(KB - 1) + Kv4Fmt<HD>::kBytes;
+  static constexpr int kRing = kAttn4Warps * kRingLen * kStage;
+  static constexpr int kOutLd = HD + 4;                              // a column's outputs, then its maximum and denominator
+  static constexpr bool kOutInRing = 8 * kOutLd * 4 * NT <= kStage;  // a warp's results fit the stage that it has read last
+  static constexpr int kOut = kOutInRing ? 0 : kAttn4Warps * 8 * NT * kOutLd * 4;
+  static constexpr int kFixed = kRing + kOut + kAttn4Batch * (int)sizeof(Unit4);   // + (B + 1) ints
+  // blocks of an SM: three fit the shared memory; what needs more than 168 registers runs two
+  static constexpr int kResident = NT == 1 && sizeof(T) == 2 ? 3 : 2;
 };
 
 struct Attn4Params {
@@ -388,13 +476,19 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same from zero: no registers have to be cleared for it
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
@@ -403,7 +497,6 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 }
 // x in (-2^15, 2^15) rounded to a multiple of 16: 11 bits on a common grid
 __device__ __forceinline__ float grid16(float x) { return __fsub_rn(__fadd_rn(x, 201326592.f), 201326592.f); }   // 1.5 * 2^27: its unit is 16
-__device__ __forceinline__ float2 half2_vals(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 // Lengths of a sequence as the kernels use them: nothing in lens, cu or the table can lead out of the buffers.
@@ -426,8 +519,7 @@ __device__ __forceinline__ Seq4 seq4(const Kv4Attn &a, int b) {
 }
 __device__ __forceinline__ int seq4_visible(int ahead, int cap, int i) { return min(max(ahead + i + 1, 0), cap); }   // keys that row i sees
 
-template <int NT>
-__device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, int x, int y) {
+__device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, int tile, int x, int y) {
   Unit4 u;
   u.b = find_seq(uoff, p.a.B, x);
   const Seq4 s = seq4(p.a, u.b);
@@ -435,13 +527,14 @@ __device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, in
   u.l = y / p.a.Hkv;
   const int nchb = max((s.cap + p.chunk - 1) / p.chunk, 1), w = x - uoff[u.b];
   u.c = w % nchb;
-  u.r0 = (w / nchb) * (8 * NT);
-  u.nrows = min(s.T * p.G - u.r0, 8 * NT);
+  u.r0 = (w / nchb) * tile;
+  u.nrows = min(s.T * p.G - u.r0, tile);
   u.tok0 = s.row0; u.ahead = s.len - s.T; u.cap = s.cap;
-  const int vis = seq4_visible(u.ahead, u.cap, (u.r0 + u.nrows - 1) / p.G);   // the tile's last row sees most
-  u.nch = max((vis + p.chunk - 1) / p.chunk, 1);
+  u.vis0 = seq4_visible(u.ahead, u.cap, u.r0 / p.G);
+  u.vis1 = seq4_visible(u.ahead, u.cap, (u.r0 + u.nrows - 1) / p.G);
+  u.nch = max((u.vis1 + p.chunk - 1) / p.chunk, 1);
   u.k0 = u.c * p.chunk;
-  u.kend = min(u.k0 + p.chunk, vis);
+  u.kend = min(u.k0 + p.chunk, u.vis1);
   return u;
 }
 
@@ -463,24 +556,38 @@ __device__ __forceinline__ float code_offset(uint32_t par) {
   const float m = __uint_as_float(par & 0xffff0000u);
   return CENTRED ? fmaf(8.f, __uint_as_float(par << 16), m) : m;
 }
+__device__ __forceinline__ float code_scale(uint32_t par) { return __uint_as_float(par << 16); }
 
-// blocks of an SM: three fit the shared memory; what needs more than 168 registers runs two
-template <typename T, int NT>
-constexpr int kAttn4Resident = NT == 1 && sizeof(T) == 2 ? 3 : 2;
+// N consecutive words from shared memory (N = 1, 2 or 4)
+template <int N>
+__device__ __forceinline__ void lds_words(const unsigned char *at, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(at);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(at);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t *>(at);
+  }
+}
 
-template <typename T, int HD, int NT>
-static __global__ void __launch_bounds__(kAttn4Threads, (kAttn4Resident<T, NT>)) k_kv4_attn(const __grid_constant__ Attn4Params p) {
+template <typename T, int HD, int RW, int NT>
+static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>::kResident)) k_kv4_attn(const __grid_constant__ Attn4Params p) {
   typedef Kv4Fmt<HD> F;
-  typedef Attn4Smem<HD, NT> S;
+  typedef Attn4Cfg<T, HD, RW, NT> S;
   constexpr int NG = F::NG, KS = 4;                       // matrix steps of 16 features per group
+  constexpr int SUB = S::SUB, KB = S::KB, NSET = S::NSET, kTile = RW * NT;
   constexpr int NSP = sizeof(T) == 4 ? 2 : 1;             // fp16 terms of a query element and of a probability
   constexpr bool CEN = NSP == 2;                          // codes as c - 8
   constexpr float kLow = CEN ? 1.f : 16777216.f, kHigh = CEN ? 1.f : 1048576.f;   // what a product with a low / high code is multiplied by
   constexpr float kHighQ = kLow == kHigh ? 1.f : 0.0625f;                         // query elements that meet high codes
   extern __shared__ __align__(16) unsigned char attn4_sm[];
+  __shared__ int s_tmp[kAttn4Warps];                      // scan totals; later, where each warp left its results
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  unsigned char *ring = attn4_sm + warp * kAttn4Ring * S::kStage;
-  float *om = reinterpret_cast<float *>(attn4_sm + S::kRing);
+  const int ka = (g & 1) * 4 + (g >> 1);                  // kappa(g): this lane's score rows are keys ka and ka + 8 of a block
+  const int sub = 2 * t / RW;                             // whose block of a set this lane's columns 2t, 2t + 1 stand for
+  unsigned char *ring = attn4_sm + warp * S::kRingLen * S::kStage;
   Unit4 *units = reinterpret_cast<Unit4 *>(attn4_sm + S::kRing + S::kOut);
   int *uoff = reinterpret_cast<int *>(attn4_sm + S::kFixed);
   const Kv4Attn &a = p.a;
@@ -488,14 +595,13 @@ static __global__ void __launch_bounds__(kAttn4Threads, (kAttn4Resident<T, NT>))
 
   // ---- the list of units: exclusive prefix sum over the sequences of (row tiles x chunks) ----
   {
-    __shared__ int wsum[kAttn4Warps];
     int carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += kAttn4Threads) {
       const int b = b0 + tid;
       int n = 0;
       if (b < a.B) {
         const Seq4 s = seq4(a, b);
-        n = ((s.T * p.G + 8 * NT - 1) / (8 * NT)) * max((s.cap + p.chunk - 1) / p.chunk, 1);
+        n = ((s.T * p.G + kTile - 1) / kTile) * max((s.cap + p.chunk - 1) / p.chunk, 1);
       }
       int v = n;
 #pragma unroll
@@ -503,13 +609,13 @@ static __global__ void __launch_bounds__(kAttn4Threads, (kAttn4Resident<T, NT>))
         const int z = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += z;
       }
-      if (lane == 31) wsum[warp] = v;
+      if (lane == 31) s_tmp[warp] = v;
       __syncthreads();
       int before = carry;
 #pragma unroll
       for (int i = 0; i < kAttn4Warps; ++i) {
-        if (i < warp) before += wsum[i];
-        carry += wsum[i];
+        if (i < warp) before += s_tmp[i];
+        carry += s_tmp[i];
       }
       if (b < a.B) uoff[b] = before + v - n;
       __syncthreads();
@@ -523,457 +629,477 @@ static __global__ void __launch_bounds__(kAttn4Threads, (kAttn4Resident<T, NT>))
   if (u0 >= u1) return;
 
   const int bpp = a.page / kKv4Block, page_sh = 31 - __clz(a.page);
+  const bool whole = a.page >= S::kKeys;   // a stage lies within a page
   const size_t page_bytes = (size_t)a.Hkv * bpp * F::kBytes;
   int q_b = -1, q_y = -1, q_r0 = -1;       // whose query rows the fragments hold
   uint32_t qf[NT][NSP][NG * KS][2];
-  float qfac[NT][2], qsum[NT][2][NG];      // of this thread's two columns: power-of-two factor with the scale, scaled feature sums
+  float qfac[NT][2], qsum[NT][2][NG];      // of this lane's two columns: power-of-two factor with the scale, scaled feature sums
 
   for (long long first = u0; first < u1; first += kAttn4Batch) {
-  const int nu = (int)min(u1 - first, (long long)kAttn4Batch);
-  if (first != u0) __syncthreads();        // every warp is done with the batch before
-  if (tid < nu) units[tid] = unit4<NT>(p, uoff, (int)((first + tid) % U), (int)((first + tid) / U));
-  __syncthreads();
+    const int nu = (int)min(u1 - first, (long long)kAttn4Batch);
+    if (first != u0) __syncthreads();      // every warp is done with the batch before
+    if (tid < nu) units[tid] = unit4(p, uoff, kTile, (int)((first + tid) % U), (int)((first + tid) / U));
+    __syncthreads();
 
-  // ---- copy side: this warp's stages in order, kAttn4Ring - 1 of them ahead of the arithmetic ----
-  int pu = 0, pi = 0, pn = 0, pk0 = 0, ent = -1, slot_w = 0;
-  const uint8_t *pbase = nullptr;          // the unit's layer and head within page 0
-  auto enter = [&]() {                     // stages of unit pu, and the page of each of their 16-key blocks (lane 2 i + j: block j of stage i)
-    const Unit4 &u = units[pu];
-    const int kend = u.kend;
-    pk0 = u.k0; pi = 0;
-    const int ns = (max(kend - pk0, 0) + kAttn4Stage - 1) / kAttn4Stage;
-    pn = (ns - warp + kAttn4Warps - 1) / kAttn4Warps;
-    pbase = a.pool + (size_t)u.l * a.pool_ls + (size_t)u.h * bpp * F::kBytes;
-    ent = -1;
-    const int key = pk0 + ((lane >> 1) * kAttn4Warps + warp) * kAttn4Stage + (lane & 1) * kKv4Block;
-    if ((lane >> 1) < pn && key < kend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
-  };
-  enter();
-  auto copy_next = [&]() {                 // request the next stage (if any); always closes a group
-    while (pi >= pn && pu < nu)
-      if (++pu < nu) enter();
-    if (pu < nu) {
-      constexpr int NC = F::kBytes / 16;   // 16-byte pieces of a block; piece c = lane + 32 i of the stage
-      unsigned char *dst = ring + slot_w * S::kStage + lane * 16;
-      const int key = pk0 + (pi * kAttn4Warps + warp) * kAttn4Stage;
-      const uint8_t *src[2];
-      bool ok[2];
+    // ---- copy side: this warp's stages in order, kRingLen - 1 of them ahead of the arithmetic ----
+    int pu = 0, pi = 0, pn = 0, pk0 = 0, ent = -1, slot_w = 0;
+    const uint8_t *pbase = nullptr;        // the unit's layer and head within page 0
+    auto enter = [&]() {                   // stages of unit pu, and the page of each of their blocks (lane KB i + j: block j of stage i)
+      const Unit4 &u = units[pu];
+      const int kend = u.kend;
+      pk0 = u.k0; pi = 0;
+      const int ns = (max(kend - pk0, 0) + S::kKeys - 1) / S::kKeys;
+      pn = (ns - warp + kAttn4Warps - 1) / kAttn4Warps;
+      pbase = a.pool + (size_t)u.l * a.pool_ls + (size_t)u.h * bpp * F::kBytes;
+      ent = -1;
+      const int key = pk0 + ((lane / KB) * kAttn4Warps + warp) * S::kKeys + (lane % KB) * kKv4Block;
+      if (lane / KB < pn && key < kend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
+    };
+    enter();
+    auto copy_next = [&]() {               // request the next stage (if any); always closes a group
+      while (pi >= pn && pu < nu)
+        if (++pu < nu) enter();
+      if (pu < nu) {
+        constexpr int NC = F::kBytes / 16;   // 16-byte pieces of a block; piece c = lane + 32 i of the stage
+        unsigned char *dst = ring + slot_w * S::kStage + lane * 16;
+        const int key = pk0 + (pi * kAttn4Warps + warp) * S::kKeys;
+        const uint8_t *src[KB];
+        bool ok[KB];
+        if (whole) {                         // one page: what follows the last key is copied too and masked with it
+          const int e = __shfl_sync(0xffffffffu, ent, KB * pi);
+          ok[0] = (unsigned)e < (unsigned)a.n_pages;
+          src[0] = pbase + (ok[0] ? (size_t)e * page_bytes : 0) + (key & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int e = __shfl_sync(0xffffffffu, ent, 2 * pi + j);
-        ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
-        src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + ((key + 16 * j) & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16 - j * F::kBytes;
+          for (int j = 1; j < KB; ++j) { ok[j] = ok[0]; src[j] = src[0]; }
+        } else
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+          const int e = __shfl_sync(0xffffffffu, ent, KB * pi + j);
+          ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
+          src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + ((key + 16 * j) & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16 - j * F::kBytes;
+        }
+#pragma unroll
+        for (int i = 0; i < (KB * NC + 31) / 32; ++i) {
+          constexpr int last = KB - 1;
+          const int j0 = 32 * i / NC, j1 = (32 * i + 31) / NC < last ? (32 * i + 31) / NC : last;
+          const bool up = j1 > j0 && lane >= j1 * NC - 32 * i;
+          if (32 * i + 31 < KB * NC || lane < KB * NC - 32 * i)
+            cp_async16(dst + 512 * i + (up ? S::block_at(j1) - j1 * F::kBytes : S::block_at(j0) - j0 * F::kBytes), (up ? src[j1] : src[j0]) + 512 * i,
+                       up ? ok[j1] : ok[j0]);
+        }
+        ++pi;
+        slot_w = slot_w + 1 == S::kRingLen ? 0 : slot_w + 1;
       }
+      cp_async_commit();
+    };
 #pragma unroll
-      for (int i = 0; i < (2 * NC + 31) / 32; ++i) {
-        const bool j = 32 * i >= NC ? true : 32 * i + 31 < NC ? false : lane >= NC - 32 * i;
-        if (32 * i + 31 < 2 * NC || lane < 2 * NC - 32 * i) cp_async16(dst + 512 * i, (j ? src[1] : src[0]) + 512 * i, j ? ok[1] : ok[0]);
-      }
-      ++pi;
-      slot_w = slot_w + 1 == kAttn4Ring ? 0 : slot_w + 1;
-    }
-    cp_async_commit();
-  };
-#pragma unroll
-  for (int i = 0; i < kAttn4Ring - 1; ++i) copy_next();
+    for (int i = 0; i < S::kRingLen - 1; ++i) copy_next();
 
-  // ---- arithmetic ----
-  int slot_r = 0;
-  for (int cu = 0; cu < nu; ++cu) {
-    const Unit4 u = units[cu];
-    if (u.b != q_b || u.l * a.Hkv + u.h != q_y || u.r0 != q_r0) {
-      q_b = u.b; q_y = u.l * a.Hkv + u.h; q_r0 = u.r0;
+    // ---- arithmetic ----
+    int slot_r = 0;
+    for (int cu = 0; cu < nu; ++cu) {
+      const Unit4 u = units[cu];
+      if (u.b != q_b || u.l * a.Hkv + u.h != q_y || u.r0 != q_r0) {
+        q_b = u.b; q_y = u.l * a.Hkv + u.h; q_r0 = u.r0;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 8 + g;          // fragment column g: row r of the tile
-        float x[NG][16];
-        if (r < u.nrows) {
-          const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
-          const T *src = (const T *)a.q + (size_t)u.l * a.q_ls + (size_t)tok * a.q_ts + (size_t)hq * a.q_hs + 16 * t;
+        for (int nt = 0; nt < NT; ++nt) {
+          const int r = nt * 8 + g % RW;     // fragment column g: row r of the tile
+          float x[NG][16];
+          if (r < u.nrows) {
+            const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
+            const T *src = (const T *)a.q + (size_t)u.l * a.q_ls + (size_t)tok * a.q_ts + (size_t)hq * a.q_hs + 16 * t;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              float y[8];
+              load8<T>(src + n * kKv4Group, p.vec, y);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[n][i] = y[i];
+              load8<T>(src + n * kKv4Group + 8, p.vec, y);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[n][8 + i] = y[i];
+            }
+          } else {
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+          }
+          float top = 0.f, sum[NG];
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            float y[8];
-            load8<T>(src + n * kKv4Group, p.vec, y);
+            sum[n] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[n][i] = y[i];
-            load8<T>(src + n * kKv4Group + 8, p.vec, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[n][8 + i] = y[i];
+            for (int i = 0; i < 16; ++i) { top = max_nan(top, fabsf(x[n][i])); sum[n] += x[n][i]; }
           }
-        } else {
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) {
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+            for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
+          }
+          // power of two that brings the row's largest element to [2^14, 2^15); a row with an infinity or a NaN makes its scores NaN
+          int e = (int)(__float_as_uint(top) >> 23) - 127;
+          const bool odd = e == 128;
+          e = min(max(e, -112), 126);
+          const float f = pow2(14 - e);
 #pragma unroll
           for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
-        }
-        float top = 0.f, sum[NG];
+            for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          sum[n] = 0.f;
+              for (int h = 0; h < 2; ++h) {
+                const float *y = &x[n][8 * w + 2 * h];   // features 2h, 2h + 4 meet low codes, 2h + 1, 2h + 5 high ones
+                float v[4] = {y[0] * f, y[4] * f, y[1] * f * kHighQ, y[5] * f * kHighQ};
 #pragma unroll
-          for (int i = 0; i < 16; ++i) { top = max_nan(top, fabsf(x[n][i])); sum[n] += x[n][i]; }
-        }
+                for (int sp = 0; sp < NSP; ++sp) {
+                  uint32_t (&dst)[2] = qf[nt][sp][n * KS + 2 * w + h];
+                  float x4[4];
 #pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-#pragma unroll
-          for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
-        }
-        // power of two that brings the row's largest element to [2^14, 2^15); a row with an infinity or a NaN makes its scores NaN
-        int e = (int)(__float_as_uint(top) >> 23) - 127;
-        const bool odd = e == 128;
-        e = min(max(e, -112), 126);
-        const float f = pow2(14 - e);
-#pragma unroll
-        for (int n = 0; n < NG; ++n)
-#pragma unroll
-          for (int w = 0; w < 2; ++w)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float *y = &x[n][8 * w + 2 * h];   // features 2h, 2h+4 (low code of a byte pair) and 2h+1, 2h+5 (high: c 2^-20)
-              float v[4] = {y[0] * f, y[4] * f, y[1] * f * kHighQ, y[5] * f * kHighQ};
-#pragma unroll
-              for (int sp = 0; sp < NSP; ++sp) {
-                uint32_t (&dst)[2] = qf[nt][sp][n * KS + 2 * w + h];
-                float u[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  u[i] = sp + 1 < NSP ? grid16(v[i]) : v[i];
-                  v[i] -= u[i];
+                  for (int i = 0; i < 4; ++i) {
+                    x4[i] = sp + 1 < NSP ? grid16(v[i]) : v[i];
+                    v[i] -= x4[i];
+                  }
+                  dst[0] = half2_bits(x4[0], x4[1]);
+                  dst[1] = half2_bits(x4[2], x4[3]);
                 }
-                dst[0] = half2_bits(u[0], u[1]);
-                dst[1] = half2_bits(u[2], u[3]);
               }
-            }
-        // scores: fac * (s_0 acc_0 + s_1 acc_1)
-        const float fac = odd ? __uint_as_float(0x7fc00000u) : p.qk_scale * kLow * pow2(e - 14);
+          // scores: fac * (s_0 acc_0 + s_1 acc_1) + ...
+          const float fac = odd ? __uint_as_float(0x7fc00000u) : p.qk_scale * kLow * pow2(e - 14);
+#pragma unroll
+          for (int col = 0; col < 2; ++col) {
+            qfac[nt][col] = __shfl_sync(0xffffffffu, fac, 4 * (2 * t + col));
+#pragma unroll
+            for (int n = 0; n < NG; ++n) qsum[nt][col][n] = __shfl_sync(0xffffffffu, sum[n] * p.qk_scale, 4 * (2 * t + col));
+          }
+        }
+      }
+      int vis[NT][2];                        // keys each of this lane's columns may see
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int col = 0; col < 2; ++col)
+          vis[nt][col] = u.vis0 == u.vis1 ? u.vis0 : seq4_visible(u.ahead, u.cap, (u.r0 + min(nt * 8 + (2 * t + col) % RW, u.nrows - 1)) / p.G);
+
+      float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
+      float lim[NG], pf[NG];                 // E = exponent of the largest value scale so far: 2^(E + 1), 2^(14 - E)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int col = 0; col < 2; ++col) {
-          qfac[nt][col] = __shfl_sync(0xffffffffu, fac, 4 * (2 * t + col));
+          m[nt][col] = -INFINITY; den[nt][col] = 0.f;
 #pragma unroll
-          for (int n = 0; n < NG; ++n) qsum[nt][col][n] = __shfl_sync(0xffffffffu, sum[n] * p.qk_scale, 4 * (2 * t + col));
+          for (int n = 0; n < NG; ++n) low[nt][col][n] = 0.f;
         }
-      }
-    }
-    int vis[NT][2];                        // keys each of this thread's columns sees
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int col = 0; col < 2; ++col) vis[nt][col] = seq4_visible(u.ahead, u.cap, (u.r0 + min(nt * 8 + 2 * t + col, u.nrows - 1)) / p.G);
-    const int vis_min = seq4_visible(u.ahead, u.cap, u.r0 / p.G);
-
-    float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
-    float lim[NG], pf[NG];                  // E = exponent of the largest value scale so far: 2^(E + 1), 2^(14 - E)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int col = 0; col < 2; ++col) {
-        m[nt][col] = -INFINITY; den[nt][col] = 0.f;
-#pragma unroll
-        for (int n = 0; n < NG; ++n) low[nt][col][n] = 0.f;
+        for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
       }
 #pragma unroll
-      for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
-    }
-#pragma unroll
-    for (int n = 0; n < NG; ++n) { lim[n] = pow2(-99); pf[n] = pow2(114); }
+      for (int n = 0; n < NG; ++n) { lim[n] = pow2(-99); pf[n] = pow2(114); }
 
-    const int ns = (max(u.kend - u.k0, 0) + kAttn4Stage - 1) / kAttn4Stage;
-    for (int si = warp; si < ns; si += kAttn4Warps) {
-      const int key0 = u.k0 + si * kAttn4Stage;
-      cp_async_wait<kAttn4Ring - 2>();
-      __syncwarp();    // the stage is there for every lane, and every lane has read the stage before it
-      copy_next();     // ... whose place is filled again
-      const unsigned char *stage = ring + slot_r * S::kStage;
-      slot_r = slot_r + 1 == kAttn4Ring ? 0 : slot_r + 1;
-      const int ka = (g & 1) * 4 + (g >> 1);            // kappa(g): this thread's score rows are keys ka and ka + 8 of a block
-      // EDGE: some row does not see all of the stage.  A key that a row does not see may hold a NaN (a later token, or whatever
-      // the page held before): it is kept out of the sums by selection, not by a weight of zero.
-      auto stage_body = [&](auto edge_c) {
-      constexpr bool EDGE = decltype(edge_c)::value;
-
-      // scores of 2 x 16 keys
-      float sc[NT][2][4];
+      const int ns = (max(u.kend - u.k0, 0) + S::kKeys - 1) / S::kKeys;
+      for (int si = warp; si < ns; si += kAttn4Warps) {
+        const int key0 = u.k0 + si * S::kKeys;
+        cp_async_wait<S::kRingLen - 2>();
+        __syncwarp();    // the stage is there for every lane, and every lane has read the stage before it
+        copy_next();     // ... whose place is filled again
+        const unsigned char *stage = ring + slot_r * S::kStage;
+        slot_r = slot_r + 1 == S::kRingLen ? 0 : slot_r + 1;
+        const unsigned char *mine = stage + S::block_at(sub);   // this lane's block of set 0 (of set k: block_at(k SUB) further)
+        const int my_key = key0 + 16 * sub + ka;
+        // EDGE: some row does not see all of the stage.  A key that a row does not see may hold a NaN (a later token, or whatever
+        // the page held before): it is kept out of the sums by selection, not by a weight of zero.
+        auto stage_body = [&](auto edge_c) {
+          constexpr bool EDGE = decltype(edge_c)::value;
+          // products of the queries with the codes of KB x 16 keys, each lane those of its columns
+          float d[NSET][NT][NG][4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const unsigned char *blk = stage + j * F::kBytes;
-        uint32_t wa[2 * NG], wb[2 * NG], pa[NG], pb[NG];
-        if (NG == 2) {
-          const uint4 va = *reinterpret_cast<const uint4 *>(blk + F::KC + ka * F::kCodes + t * 16);
-          const uint4 vb = *reinterpret_cast<const uint4 *>(blk + F::KC + (ka + 8) * F::kCodes + t * 16);
-          wa[0] = va.x; wa[1] = va.y; wa[2 * NG - 2] = va.z; wa[2 * NG - 1] = va.w;
-          wb[0] = vb.x; wb[1] = vb.y; wb[2 * NG - 2] = vb.z; wb[2 * NG - 1] = vb.w;
-          const uint2 qa = *reinterpret_cast<const uint2 *>(blk + F::KP + ka * F::kPar), qb = *reinterpret_cast<const uint2 *>(blk + F::KP + (ka + 8) * F::kPar);
-          pa[0] = qa.x; pa[NG - 1] = qa.y; pb[0] = qb.x; pb[NG - 1] = qb.y;
-        } else {
-          const uint2 va = *reinterpret_cast<const uint2 *>(blk + F::KC + ka * F::kCodes + t * 8);
-          const uint2 vb = *reinterpret_cast<const uint2 *>(blk + F::KC + (ka + 8) * F::kCodes + t * 8);
-          wa[0] = va.x; wa[1] = va.y; wb[0] = vb.x; wb[1] = vb.y;
-          pa[0] = *reinterpret_cast<const uint32_t *>(blk + F::KP + ka * F::kPar);
-          pb[0] = *reinterpret_cast<const uint32_t *>(blk + F::KP + (ka + 8) * F::kPar);
-        }
-        float d[NT][NSP][NG][4];
+          for (int j = 0; j < KB; ++j) {
+            const unsigned char *blk = stage + S::block_at(j);
+            uint32_t wa[2 * NG], wb[2 * NG];
+            lds_words(blk + F::KC + ka * F::kCodes + t * 8 * NG, wa);
+            lds_words(blk + F::KC + (ka + 8) * F::kCodes + t * 8 * NG, wb);
+            float x[NT][NSP][NG][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int n = 0; n < NG; ++n)
 #pragma unroll
-          for (int sp = 0; sp < NSP; ++sp)
+              for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int n = 0; n < NG; ++n) d[nt][sp][n][0] = d[nt][sp][n][1] = d[nt][sp][n][2] = d[nt][sp][n][3] = 0.f;
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t y = wa[2 * n + w] >> (8 * h), z = wb[2 * n + w] >> (8 * h);
+                  const uint32_t a0 = code_pair<CEN, 0>(y), a1 = code_pair<CEN, 0>(z), a2 = code_pair<CEN, 1>(y), a3 = code_pair<CEN, 1>(z);
 #pragma unroll
-        for (int n = 0; n < NG; ++n)
+                  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int w = 0; w < 2; ++w)
+                    for (int sp = 0; sp < NSP; ++sp) {
+                      const uint32_t (&q2)[2] = qf[nt][sp][n * KS + 2 * w + h];
+                      if (w == 0 && h == 0) mma_f16_first(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
+                      else mma_f16(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
+                    }
+                }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t x = wa[2 * n + w] >> (8 * h), y = wb[2 * n + w] >> (8 * h);
-              const uint32_t a0 = code_pair<CEN, 0>(x), a1 = code_pair<CEN, 0>(y), a2 = code_pair<CEN, 1>(x), a3 = code_pair<CEN, 1>(y);
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float y = NSP == 1 ? x[nt][0][n][i] : x[nt][0][n][i] + x[nt][NSP - 1][n][i];
+                  float &to = d[j / SUB][nt][n][i];
+                  to = j % SUB == 0 ? y : sub == j % SUB ? y : to;
+                }
+          }
+          // scores
+          float sc[NSET][NT][4];
+#pragma unroll
+          for (int k = 0; k < NSET; ++k)
+#pragma unroll
+            for (int row = 0; row < 2; ++row) {
+              uint32_t par[NG];
+              lds_words(mine + S::block_at(k * SUB) + F::KP + (ka + 8 * row) * F::kPar, par);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int sp = 0; sp < NSP; ++sp) mma_f16(d[nt][sp][n], a0, a1, a2, a3, qf[nt][sp][n * KS + 2 * w + h][0], qf[nt][sp][n * KS + 2 * w + h][1]);
+                for (int col = 0; col < 2; ++col) {
+                  float dot = 0.f, off = 0.f;
+#pragma unroll
+                  for (int n = 0; n < NG; ++n) {
+                    dot = fmaf(code_scale(par[n]), d[k][nt][n][2 * row + col], dot);
+                    off = fmaf(code_offset<CEN>(par[n]), qsum[nt][col][n], off);
+                  }
+                  float s = fmaf(qfac[nt][col], dot, off);
+                  if (EDGE && my_key + 16 * SUB * k + 8 * row >= vis[nt][col]) s = -INFINITY;
+                  sc[k][nt][2 * row + col] = s;
+                }
             }
+
+          // value parameters of this lane's keys; keys that no row of the tile sees count as zeros
+          uint32_t vp[NSET][2][NG];
+          float top[NG], grow[NG];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int n = 0; n < NG; ++n) { top[n] = 0.f; grow[n] = 1.f; }
 #pragma unroll
-          for (int row = 0; row < 2; ++row)
+          for (int k = 0; k < NSET; ++k)
 #pragma unroll
-            for (int col = 0; col < 2; ++col) {
-              float dot = 0.f, off = 0.f;
+            for (int row = 0; row < 2; ++row) {
+              lds_words(mine + S::block_at(k * SUB) + F::VP + (ka + 8 * row) * F::kPar, vp[k][row]);
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
-                const uint32_t par = row ? pb[n] : pa[n];
-                dot = fmaf(__uint_as_float(par << 16), NSP == 1 ? d[nt][0][n][2 * row + col] : d[nt][0][n][2 * row + col] + d[nt][NSP - 1][n][2 * row + col], dot);
-                off = fmaf(code_offset<CEN>(par), qsum[nt][col][n], off);
+                if (EDGE && my_key + 16 * SUB * k + 8 * row >= u.kend) vp[k][row][n] = 0u;
+                top[n] = fmaxf(top[n], code_scale(vp[k][row][n]));   // (passes over a NaN)
               }
-              float s = fmaf(qfac[nt][col], dot, off);
-              if (EDGE && key0 + 16 * j + ka + 8 * row >= vis[nt][col]) s = -INFINITY;
-              sc[nt][j][2 * row + col] = s;
             }
+          // a scale of 2^(E + 1) or more raises E
+          bool rescale = false;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) rescale = rescale || top[n] >= lim[n];
+          rescale = __any_sync(0xffffffffu, rescale);
+          if (rescale) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              const int was = (int)(__float_as_uint(lim[n]) >> 23) - 128;
+              const int e = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top[n])) >> 23) - 127, was), 126);
+              grow[n] = pow2(max(was - e, -126));
+              lim[n] = pow2(e + 1);
+              pf[n] = pow2(14 - e);
+            }
+          }
+
+          // running maximum, probabilities
+          float alpha[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int col = 0; col < 2; ++col) {
+              float x = fmaxf(sc[0][nt][col], sc[0][nt][2 + col]);
+#pragma unroll
+              for (int k = 1; k < NSET; ++k) x = fmaxf(x, fmaxf(sc[k][nt][col], sc[k][nt][2 + col]));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+              x = fmaxf(x, m[nt][col]);
+              const float ref = x == -INFINITY ? 0.f : x;   // nothing visible yet: every probability below is exp2(-inf) = 0
+              alpha[nt][col] = ex2(m[nt][col] - ref);
+              rescale = rescale || x != m[nt][col];
+              m[nt][col] = x;
+              float sum = 0.f, lo[NG];
+#pragma unroll
+              for (int n = 0; n < NG; ++n) lo[n] = 0.f;
+#pragma unroll
+              for (int k = 0; k < NSET; ++k)
+#pragma unroll
+                for (int row = 0; row < 2; ++row) {
+                  const float pr = ex2(sc[k][nt][2 * row + col] - ref);
+                  sc[k][nt][2 * row + col] = pr;
+                  sum += pr;
+#pragma unroll
+                  for (int n = 0; n < NG; ++n) {
+                    const float off = code_offset<CEN>(vp[k][row][n]);
+                    if (!EDGE || my_key + 16 * SUB * k + 8 * row < vis[nt][col]) lo[n] = fmaf(pr, off, lo[n]);
+                  }
+                }
+              den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
+#pragma unroll
+              for (int n = 0; n < NG; ++n) low[nt][col][n] = fmaf(low[nt][col][n], alpha[nt][col], lo[n]);
+            }
+          if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int n = 0; n < NG; ++n) {
+                const float f0 = alpha[nt][0] * grow[n], f1 = alpha[nt][1] * grow[n];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  acc[nt][n * 4 + i][0] *= f0; acc[nt][n * 4 + i][1] *= f1; acc[nt][n * 4 + i][2] *= f0; acc[nt][n * 4 + i][3] *= f1;
+                }
+              }
+          }
+
+          // p s as the 8-column operand of the second product: rows 2t, 2t + 1 (+ 8) of column g
+          uint32_t b[NSET][NG][NT][NSP][2];
+#pragma unroll
+          for (int k = 0; k < NSET; ++k)
+#pragma unroll
+            for (int row = 0; row < 2; ++row)
+#pragma unroll
+              for (int n = 0; n < NG; ++n) {
+                const float s = code_scale(vp[k][row][n]) * pf[n];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  float x0 = sc[k][nt][2 * row] * s, x1 = sc[k][nt][2 * row + 1] * s;
+                  if (EDGE) {
+                    const int key = my_key + 16 * SUB * k + 8 * row;
+                    x0 = key >= vis[nt][0] ? 0.f : x0;
+                    x1 = key >= vis[nt][1] ? 0.f : x1;
+                  }
+                  if (NSP == 2) {
+                    const float h0 = grid16(x0), h1 = grid16(x1);
+                    b[k][n][nt][0][row] = transpose8(half2_bits(h0, h1));
+                    b[k][n][nt][NSP - 1][row] = transpose8(half2_bits(x0 - h0, x1 - h1));
+                  } else {
+                    b[k][n][nt][0][row] = transpose8(half2_bits(x0, x1));
+                  }
+                }
+              }
+          // o += (p s) c
+#pragma unroll
+          for (int j = 0; j < KB; ++j) {
+            const unsigned char *blk = stage + S::block_at(j) + F::VC + g * 4 * NG;
+            uint32_t v[4][NG];               // words of features 8g .. 8g + 7 of the groups, of keys t, t + 4, t + 8, t + 12
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lds_words(blk + (t + 4 * i) * F::kCodes, v[i]);
+            const bool on = SUB == 1 || g / RW == j % SUB;   // column g holds this block's keys
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              uint32_t bj[NT][NSP][2];
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int sp = 0; sp < NSP; ++sp)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) bj[nt][sp][i] = on ? b[j / SUB][n][nt][sp][i] : 0u;
+#pragma unroll
+              for (int hi = 0; hi < 2; ++hi) {
+                const uint32_t x = __byte_perm(v[0][n], v[1][n], hi ? 0x7632 : 0x5410), y = __byte_perm(v[2][n], v[3][n], hi ? 0x7632 : 0x5410);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  // a byte (16 times the high code + the low one) stands for the high code: one mask less, and the low code's sum,
+                  // which is in the same thread, is taken off at the end
+                  const uint32_t xb = CEN ? x >> (8 * h) : h ? __byte_perm(x, 0, 0x4341) : x & 0x00ff00ffu;
+                  const uint32_t yb = CEN ? y >> (8 * h) : h ? __byte_perm(y, 0, 0x4341) : y & 0x00ff00ffu;
+                  const uint32_t a0 = code_pair<CEN, 0>(xb), a1 = CEN ? code_pair<CEN, 1>(xb) : xb;
+                  const uint32_t a2 = code_pair<CEN, 0>(yb), a3 = CEN ? code_pair<CEN, 1>(yb) : yb;
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) {
+                    float (&o)[4] = acc[nt][n * 4 + 2 * hi + h];
+                    if (NSP == 1) {
+                      mma_f16(o, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
+                    } else {
+                      float e0[4], e1[4];
+                      mma_f16_first(e0, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
+                      mma_f16_first(e1, a0, a1, a2, a3, bj[nt][NSP - 1][0], bj[nt][NSP - 1][1]);
+#pragma unroll
+                      for (int i = 0; i < 4; ++i) o[i] += e0[i] + e1[i];
+                    }
+                  }
+                }
+              }
+            }
+          }
+        };
+        if (key0 + S::kKeys > u.vis0) stage_body(std::true_type{});
+        else stage_body(std::false_type{});
       }
 
-      // value parameters of this thread's four keys; keys that no row of the tile sees count as zeros
-      uint32_t vp[2][2][NG];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int row = 0; row < 2; ++row) {
-          const unsigned char *at = stage + j * F::kBytes + F::VP + (ka + 8 * row) * F::kPar;
-          if (NG == 2) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(at);
-            vp[j][row][0] = v.x; vp[j][row][NG - 1] = v.y;
-          } else {
-            vp[j][row][0] = *reinterpret_cast<const uint32_t *>(at);
-          }
-          if (EDGE && key0 + 16 * j + ka + 8 * row >= u.kend) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) vp[j][row][n] = 0u;
-          }
-        }
-      // a scale of 2^(E + 1) or more raises E (fmaxf passes over a NaN)
-      float top[NG], grow[NG];
-      bool rescale = false;
-#pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        top[n] = fmaxf(fmaxf(__uint_as_float(vp[0][0][n] << 16), __uint_as_float(vp[0][1][n] << 16)),
-                       fmaxf(__uint_as_float(vp[1][0][n] << 16), __uint_as_float(vp[1][1][n] << 16)));
-        rescale = rescale || top[n] >= lim[n];
-        grow[n] = 1.f;
-      }
-      rescale = __any_sync(0xffffffffu, rescale);
-      if (rescale) {
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          const int was = (int)(__float_as_uint(lim[n]) >> 23) - 128;
-          const int e = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top[n], 0.f))) >> 23) - 127, was), 126);
-          grow[n] = pow2(max(was - e, -126));
-          lim[n] = pow2(e + 1);
-          pf[n] = pow2(14 - e);
-        }
-      }
-
-      // running maximum, probabilities
-      float alpha[NT][2];
+      // ---- join the columns of the four warps ----
+      // a warp leaves its columns in the stage that it has read last (nothing is copied there before its next stage begins)
+      const int out_at = S::kOutInRing ? (warp * S::kRingLen + (slot_r == 0 ? S::kRingLen - 1 : slot_r - 1)) * S::kStage
+                                       : S::kRing + warp * 8 * NT * S::kOutLd * 4;
+      float *om = reinterpret_cast<float *>(attn4_sm + out_at);
+      if (S::kOutInRing) __syncwarp();   // every lane has read it
+      else if (cu != 0) __syncthreads(); // the previous unit's results have been read
+      if (lane == 0) s_tmp[warp] = out_at;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int col = 0; col < 2; ++col) {
-          float x = fmaxf(fmaxf(sc[nt][0][col], sc[nt][0][2 + col]), fmaxf(sc[nt][1][col], sc[nt][1][2 + col]));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-          x = fmaxf(x, m[nt][col]);
-          const float ref = x == -INFINITY ? 0.f : x;   // nothing visible yet: every probability below is exp2(-inf) = 0
-          alpha[nt][col] = ex2(m[nt][col] - ref);
-          rescale = rescale || x != m[nt][col];
-          m[nt][col] = x;
-          float sum = 0.f, lo[NG];
+          float l = den[nt][col], lo[NG];
 #pragma unroll
-          for (int n = 0; n < NG; ++n) lo[n] = 0.f;
+          for (int n = 0; n < NG; ++n) lo[n] = low[nt][col][n];
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int o = 4; o < 32; o <<= 1) {
+            l += __shfl_xor_sync(0xffffffffu, l, o);
 #pragma unroll
-            for (int row = 0; row < 2; ++row) {
-              const float pr = ex2(sc[nt][j][2 * row + col] - ref);
-              sc[nt][j][2 * row + col] = pr;
-              sum += pr;
-#pragma unroll
-              for (int n = 0; n < NG; ++n) {
-                const float off = code_offset<CEN>(vp[j][row][n]);
-                if (!EDGE || key0 + 16 * j + ka + 8 * row < vis[nt][col]) lo[n] = fmaf(pr, off, lo[n]);
-              }
-            }
-          den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
-#pragma unroll
-          for (int n = 0; n < NG; ++n) low[nt][col][n] = fmaf(low[nt][col][n], alpha[nt][col], lo[n]);
-        }
-      if (__any_sync(0xffffffffu, rescale)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int n = 0; n < NG; ++n) {
-            const float f0 = alpha[nt][0] * grow[n], f1 = alpha[nt][1] * grow[n];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[nt][n * 4 + i][0] *= f0; acc[nt][n * 4 + i][1] *= f1; acc[nt][n * 4 + i][2] *= f0; acc[nt][n * 4 + i][3] *= f1;
-            }
+            for (int n = 0; n < NG; ++n) lo[n] += __shfl_xor_sync(0xffffffffu, lo[n], o);
           }
-      }
-
-      // o += (p s) c
-      uint32_t v[2][4][NG];                  // words of features 8g..8g+7 of the groups, of keys t, t+4, t+8, t+12 of both blocks
+          if (nt * 8 + (2 * t + col) % RW < u.nrows) {
+            float *dst = om + (nt * 8 + 2 * t + col) * S::kOutLd;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+            for (int n = 0; n < NG; ++n) {
+              // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes, or bytes)
+              const float back = lim[n] * pow2(-15);   // 2^(E - 14)
+              float y[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned char *at = stage + j * F::kBytes + F::VC + (t + 4 * i) * F::kCodes + g * 4 * NG;
-          if (NG == 2) {
-            const uint2 x = *reinterpret_cast<const uint2 *>(at);
-            v[j][i][0] = x.x; v[j][i][NG - 1] = x.y;
+              for (int i = 0; i < 4; ++i) {
+                y[2 * i] = fmaf(acc[nt][n * 4 + i][col] * kLow, back, lo[n]);
+                const float high = CEN ? acc[nt][n * 4 + i][2 + col] : acc[nt][n * 4 + i][2 + col] - acc[nt][n * 4 + i][col];
+                y[2 * i + 1] = fmaf(high * kHigh, back, lo[n]);
+              }
+              reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[0] = make_float4(y[0], y[1], y[2], y[3]);
+              reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[1] = make_float4(y[4], y[5], y[6], y[7]);
+            }
+            if (g == 0) { dst[HD] = m[nt][col]; dst[HD + 1] = l; }
+          }
+        }
+      __syncthreads();
+      if (u.c < u.nch) {   // (a chunk that no row of the tile sees leaves nothing behind)
+        const int e = tid % HD;
+        for (int r = tid / HD; r < u.nrows; r += kAttn4Threads / HD) {
+          constexpr int NP = kAttn4Warps * SUB;   // parts of a row: warp, then block class
+          auto part = [&](int i) { return reinterpret_cast<const float *>(attn4_sm + s_tmp[i / SUB]) + (NT > 1 ? r : (i % SUB) * RW + r) * S::kOutLd; };
+          float M = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) M = fmaxf(M, part(i)[HD]);
+          const float ref = M == -INFINITY ? 0.f : M;
+          float o = 0.f, l = 0.f;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float *src = part(i);
+            const float lw = src[HD + 1], f = ex2(src[HD] - ref);
+            if (lw != 0.f) { o = fmaf(f, src[e], o); l = fmaf(f, lw, l); }   // a part that saw nothing is left out; a NaN is not
+          }
+          const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
+          const size_t row = (size_t)tok * a.Hq + hq;
+          if (u.nch == 1) {
+            ((T *)a.out)[(size_t)u.l * a.o_ls + row * HD + e] = from_f<T>(l == 0.f ? 0.f : o / l);
           } else {
-            v[j][i][0] = *reinterpret_cast<const uint32_t *>(at);
+            float *dst = a.part + (((size_t)u.l * a.n_rows * a.Hq + row) * p.nch_max + u.c) * (HD + 4);
+            dst[e] = o;
+            if (e == 0) { dst[HD] = M; dst[HD + 1] = l; }
           }
         }
-#pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        uint32_t b[2][NT][NSP][2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int row = 0; row < 2; ++row) {
-            const float s = __uint_as_float(vp[j][row][n] << 16) * pf[n];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float x0 = sc[nt][j][2 * row] * s, x1 = sc[nt][j][2 * row + 1] * s;
-              if (EDGE) {
-                const int key = key0 + 16 * j + ka + 8 * row;
-                x0 = key >= vis[nt][0] ? 0.f : x0;
-                x1 = key >= vis[nt][1] ? 0.f : x1;
-              }
-              if (NSP == 2) {
-                const float h0 = grid16(x0), h1 = grid16(x1);
-                b[j][nt][0][row] = transpose8(half2_bits(h0, h1));
-                b[j][nt][NSP - 1][row] = transpose8(half2_bits(x0 - h0, x1 - h1));
-              } else {
-                b[j][nt][0][row] = transpose8(half2_bits(x0, x1));
-              }
-            }
-          }
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t fr[2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t x = __byte_perm(v[j][0][n], v[j][1][n], hi ? 0x7632 : 0x5410) >> (8 * h);
-              const uint32_t y = __byte_perm(v[j][2][n], v[j][3][n], hi ? 0x7632 : 0x5410) >> (8 * h);
-              fr[j][0] = code_pair<CEN, 0>(x); fr[j][1] = code_pair<CEN, 1>(x); fr[j][2] = code_pair<CEN, 0>(y); fr[j][3] = code_pair<CEN, 1>(y);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float (&o)[4] = acc[nt][n * 4 + 2 * hi + h];
-              if (NSP == 1) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) mma_f16(o, fr[j][0], fr[j][1], fr[j][2], fr[j][3], b[j][nt][0][0], b[j][nt][0][1]);
-              } else {
-                float d[2][4] = {};
-#pragma unroll
-                for (int sp = 0; sp < 2; ++sp)
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) mma_f16(d[sp], fr[j][0], fr[j][1], fr[j][2], fr[j][3], b[j][nt][sp * (NSP - 1)][0], b[j][nt][sp * (NSP - 1)][1]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] += d[0][i] + d[1][i];
-              }
-            }
-          }
       }
-      };
-      if (key0 + kAttn4Stage > vis_min) stage_body(std::true_type{});
-      else stage_body(std::false_type{});
+      if (S::kOutInRing) __syncthreads();   // ... and read, before a stage is copied over it
     }
-
-    // ---- join the four warps ----
-    if (cu != 0) __syncthreads();   // the previous unit's results have been read
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int col = 0; col < 2; ++col) {
-        float l = den[nt][col], lo[NG];
-#pragma unroll
-        for (int n = 0; n < NG; ++n) lo[n] = low[nt][col][n];
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          l += __shfl_xor_sync(0xffffffffu, l, o);
-#pragma unroll
-          for (int n = 0; n < NG; ++n) lo[n] += __shfl_xor_sync(0xffffffffu, lo[n], o);
-        }
-        const int r = nt * 8 + 2 * t + col;
-        if (r < u.nrows) {
-          float *dst = om + (size_t)(warp * 8 * NT + r) * S::kOutLd;
-#pragma unroll
-          for (int n = 0; n < NG; ++n) {
-            // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes)
-            const float back = lim[n] * pow2(-15);   // 2^(E - 14)
-            float y[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              y[2 * i] = fmaf(acc[nt][n * 4 + i][col] * kLow, back, lo[n]);
-              y[2 * i + 1] = fmaf(acc[nt][n * 4 + i][2 + col] * kHigh, back, lo[n]);
-            }
-            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[0] = make_float4(y[0], y[1], y[2], y[3]);
-            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[1] = make_float4(y[4], y[5], y[6], y[7]);
-          }
-          if (g == 0) { dst[HD] = m[nt][col]; dst[HD + 1] = l; }
-        }
-      }
-    __syncthreads();
-    if (u.c < u.nch) {   // (a chunk that no row of the tile sees leaves nothing behind)
-      const int e = tid % HD;
-      for (int r = tid / HD; r < u.nrows; r += kAttn4Threads / HD) {
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kAttn4Warps; ++w) M = fmaxf(M, om[(size_t)(w * 8 * NT + r) * S::kOutLd + HD]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float o = 0.f, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kAttn4Warps; ++w) {
-          const float *src = om + (size_t)(w * 8 * NT + r) * S::kOutLd;
-          const float lw = src[HD + 1], f = lw == 0.f ? 0.f : ex2(src[HD] - ref);   // a warp that saw nothing weighs nothing; a NaN stays
-          if (lw != 0.f) { o = fmaf(f, src[e], o); l = fmaf(f, lw, l); }
-        }
-        const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
-        const size_t row = (size_t)tok * a.Hq + hq;
-        if (u.nch == 1) {
-          ((T *)a.out)[(size_t)u.l * a.o_ls + row * HD + e] = from_f<T>(l == 0.f ? 0.f : o / l);
-        } else {
-          float *dst = a.part + (((size_t)u.l * a.n_rows * a.Hq + row) * p.nch_max + u.c) * (HD + 4);
-          dst[e] = o;
-          if (e == 0) { dst[HD] = M; dst[HD + 1] = l; }
-        }
-      }
-    }
-  }
-  cp_async_wait<0>();
+    cp_async_wait<0>();
   }
 }
 

@@ -47,6 +47,7 @@ struct Kv4Attn {
   void *out; size_t o_ls;                   // [rows][Hq][hd]
   float *part;                              // workspace
   int T, n_rows, B, Hq, Hkv, hd, n_pages, page, max_len, nl;
+  int tile;                                 // query rows of a work unit: 2, 4, 8 or 16; 0 = chosen by the rows of a sequence and kv head
   float scale;
   bool fp32;
 };

@@ -680,6 +680,7 @@ static int kv4_attend(snlp_model *m, const Fwd &f, int l0, int nl, const void *q
   a.pool_ls = f.kv4->pool_ls; a.table = f.kv4->table; a.tstride = f.kv4->row_pages; a.lens = f.kv4->lens;
   a.T = f.T; a.n_rows = f.M; a.B = f.B; a.Hq = a.Hkv = c.n_head; a.hd = c.head_dim; a.n_pages = f.kv4->n_pages; a.page = kKv4Page;
   a.max_len = f.kv4->max_ctx; a.scale = 1.f / std::sqrt((float)c.head_dim); a.fp32 = c.dtype == SNLP_DTYPE_FP32;
+  a.tile = 2;   // one tile for single tokens and blocks of them, so that a verify block reproduces the decode steps bit for bit
   // the decode regime has workspace for all layers at once; more rows go layer by layer
   const bool all = f.M <= kDecodeRows;
   for (int i = 0; i < nl; i += all ? nl : 1) {

@@ -57,7 +57,7 @@ class Kv4Pool(C.Structure):
 class Kv4Attn(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("block_table", C.c_void_p), ("lens", C.c_void_p),
                 ("cu_q", C.c_void_p)] + \
-               [(n, C.c_int32) for n in ("dtype", "n_rows", "B", "n_head", "max_pages", "max_len")] + [("scale", C.c_float)]
+               [(n, C.c_int32) for n in ("dtype", "n_rows", "B", "n_head", "max_pages", "max_len", "tile_rows")] + [("scale", C.c_float)]
 
 
 class SnlpError(RuntimeError):
@@ -443,29 +443,31 @@ def kv4_read(pool: torch.Tensor, slots: torch.Tensor, head_dim: int, dtype=torch
     if k is None or v is None:
         shape = (slots.numel(), pool.shape[1], head_dim)
         k = pool.new_empty(shape, dtype=dtype) if k is None else k
-        v = pool.new_empty(shape, dtype=dtype) if v is None else v
+        v = torch.empty_like(k, memory_format=torch.contiguous_format) if v is None else v
     _kv4_rows(_lib.snlp_kv4_read, pool, k, v, slots)
     return k, v
 
 
 def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor | None = None,
-                  max_len: int = 0, scale: float | None = None, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+                  max_len: int = 0, scale: float | None = None, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                  tile_rows: int = 0) -> torch.Tensor:
     """Causal attention of q [rows, n_head, head_dim] over the pages (snlp_kv4_attention): int32 block_table [B, max_pages],
     lens [B]; cu_q [B + 1] gives each sequence's rows (None: rows / B each).  max_len: a bound of the lengths known on the
-    host (0: the table's capacity); workspace: uint8, by default allocated per call."""
+    host (0: the table's capacity); workspace: uint8, by default allocated per call; tile_rows: 2, 4, 8 or 16 rows worked on
+    together (0: chosen by the sizes), one value for calls whose rows have to agree bit for bit."""
     p, dev, shape, B, tab, i32 = _kv4_pool_arg(pool), pool.device, q.shape, lens.numel(), block_table.shape, torch.int32
     if q.device != dev or len(shape) != 3 or shape[2] != p.head_dim or (shape[0] and q.stride(2) != 1):
         _refuse("q must be [rows, n_head, head_dim] on the pool's device, features contiguous")
     if len(tab) != 2 or tab[0] != B or (cu_q is not None and cu_q.numel() != B + 1):
         _refuse("block_table must be [B, max_pages], lens [B], cu_q [B + 1]")
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape:
         _refuse("out must have q's shape")
     qt, qh, _ = q.stride()
     a = Kv4Attn(q.data_ptr(), qt, qh, _dense_ptr("block_table", block_table, i32, dev), _dense_ptr("lens", lens, i32, dev),
                 _dense_ptr("cu_q", cu_q, i32, dev) if cu_q is not None else None, _kv4_dtype(q.dtype), shape[0], B, shape[1], tab[1], max_len,
-                scale if scale is not None else 0.0)
+                tile_rows, scale if scale is not None else 0.0)
     po = _dense_ptr("out", out, q.dtype, dev)
     pp, pa, pw, size = C.byref(p), C.byref(a), None, 0
     if workspace is None:

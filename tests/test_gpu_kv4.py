@@ -347,14 +347,14 @@ def test_attention_single_token_lengths(S, n, dim, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("page", [16, 32, 64, 256])
-@pytest.mark.parametrize("hq,hk", [(1, 1), (10, 10), (8, 2), (7, 1), (24, 3), (9, 1)])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (10, 10), (4, 2), (6, 2), (8, 2), (7, 1), (24, 3), (9, 1)])
 def test_attention_heads_and_pages(S, hq, hk, page, dtype):
     run_attention(S, [300, 7, 64, 129], 1, hq, hk, 128, page, dtype, seed=page + hq)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("T", [2, 7, 8, 9, 16, 17, 40])
+@pytest.mark.parametrize("T", [2, 3, 4, 7, 8, 9, 16, 17, 40])
 def test_attention_blocks_of_rows(S, T, dim, dtype):
     run_attention(S, [T, T + 1, 270, 530], T, 4, 2, dim, 32, dtype, seed=T)
 
@@ -382,12 +382,12 @@ def test_attention_rows_behind_the_last_sequence_stay(S):
     c.check(out, q64, [0, 1, 4], BF)
 
 
-@pytest.mark.parametrize("B,n,hk", [(2, 2500, 3), (40, 700, 2), (150, 1100, 2)])     # every chunk length
-def test_attention_many_chunks(S, B, n, hk):
+@pytest.mark.parametrize("B,n,hk,G", [(2, 2500, 3, 1), (40, 700, 2, 3), (150, 1100, 2, 5)])     # every chunk length, more units than a batch
+def test_attention_many_chunks(S, B, n, hk, G):
     rng = np.random.default_rng(B)
     lens = rng.integers(1, n + 1, B).tolist()
     lens[0] = n
-    run_attention(S, lens, 1, hk, hk, 64, 64, F32)
+    run_attention(S, lens, 1, hk * G, hk, 64, 64, F32)
 
 
 def test_attention_max_len_cuts_and_scale(S):
@@ -455,22 +455,24 @@ def test_attention_nan_reaches_only_who_sees_it(S, dtype):
         assert np.isnan(got[1, 0]).all() and np.isfinite(got[[0, 2]]).all() and np.isfinite(got[1, 1]).all()
 
 
-def test_attention_row_does_not_depend_on_its_company(S):
-    """The same row bit for bit: alone, within a block, grouped differently in the call, with other lengths beside it."""
-    for dtype in (BF, F32):
-        c = Cache(S, [700], 3, 128, 64, dtype)
-        q, _ = rounded(np.random.default_rng(2), (9, 3, 128), dtype)
-        block = c.attend(q)
-        for i in (0, 3, 8):
-            one = Cache.__new__(Cache)
-            one.__dict__.update(c.__dict__)
-            one.lens = [700 - 8 + i]
-            assert torch.equal(one.attend(q[i:i + 1].contiguous())[0], block[i])
-        assert torch.equal(c.attend(q), block)
-    two, k, v = Cache(S, [700, 30], 3, 128, 64, F32), *(rounded(np.random.default_rng(i), (700, 3, 128), F32)[0] for i in (3, 4))
+@pytest.mark.parametrize("tile", [2, 4, 8, 16])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_row_does_not_depend_on_its_company(S, tile, dtype):
+    """The same row bit for bit for one tile_rows: alone, within a block, with other lengths beside it; and right for each."""
+    c = Cache(S, [700], 3, 128, 64, dtype)
+    q, q64 = rounded(np.random.default_rng(2), (9, 3, 128), dtype)
+    block = c.attend(q, tile_rows=tile)
+    c.check(block, q64, [0, 9], dtype)
+    for i in (0, 3, 8):
+        one = Cache.__new__(Cache)
+        one.__dict__.update(c.__dict__)
+        one.lens = [700 - 8 + i]
+        assert torch.equal(one.attend(q[i:i + 1].contiguous(), tile_rows=tile)[0], block[i])
+    assert torch.equal(c.attend(q, tile_rows=tile), block)
+    two, k, v = Cache(S, [700, 30], 3, 128, 64, dtype), *(rounded(np.random.default_rng(i), (700, 3, 128), dtype)[0] for i in (3, 4))
     c.put(0, 0, k, v)
     two.put(0, 0, k, v)
-    assert torch.equal(two.attend(torch.cat([q[-1:], q[:1]]))[0], c.attend(q[-1:].contiguous())[0])
+    assert torch.equal(two.attend(torch.cat([q[-1:], q[:1]]), tile_rows=tile)[0], c.attend(q[-1:].contiguous(), tile_rows=tile)[0])
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

@@ -17,7 +17,7 @@ def pool(pages=P, n_pages=4, page=16, heads=2, dim=64):
 
 
 def attn(**kw):
-    d = dict(q=P, q_token_stride=256, q_head_stride=64, block_table=P, lens=P, cu_q=None, dtype=1, n_rows=2, B=2, n_head=4, max_pages=8, max_len=0, scale=0.0)
+    d = dict(q=P, q_token_stride=256, q_head_stride=64, block_table=P, lens=P, cu_q=None, dtype=1, n_rows=2, B=2, n_head=4, max_pages=8, max_len=0, tile_rows=0, scale=0.0)
     d.update(kw)
     return snlp.Kv4Attn(*[d[n] for n, _ in snlp.Kv4Attn._fields_])
 
@@ -78,7 +78,7 @@ def test_attention():
         return lib.snlp_kv4_attention(C.byref(pl or pool()), C.byref(attn(**kw)), C.c_void_p(out), C.c_void_p(ws), C.c_size_t(size), None)
     for bad in (dict(q=None), dict(block_table=None), dict(lens=None), dict(out=0), dict(dtype=2), dict(B=0), dict(n_rows=-1), dict(n_head=3), dict(n_head=0),
                 dict(n_rows=3), dict(max_pages=0), dict(max_len=-1), dict(q=P + 1), dict(out=P + 1), dict(lens=P + 2), dict(cu_q=P + 1), dict(q_token_stride=-1),
-                dict(scale=float("nan")), dict(ws=P + 4), dict(dtype=0, q=P + 2)):
+                dict(scale=float("nan")), dict(tile_rows=1), dict(tile_rows=-2), dict(tile_rows=32), dict(ws=P + 4), dict(dtype=0, q=P + 2)):
         assert go(**bad) == snlp.ERR_ARG, bad
         assert "snlp_kv4_attention" in message()
     assert go(B=4097, n_rows=4097) == snlp.ERR_SHAPE
