@@ -19,11 +19,14 @@ cudaError_t kv4_plan(const Kv4Plan &p, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-// 16-byte accesses need every row to start on such a boundary
-static bool rows_vec(const Kv4Rows &p) {
-  const size_t u = p.fp32 ? 4 : 8;   // elements in 16 bytes
-  auto ok = [&](const void *x, size_t ls, size_t ts, size_t hs) { return (uintptr_t)x % 16 == 0 && ls % u == 0 && ts % u == 0 && hs % u == 0; };
-  return ok(p.k, p.k_ls, p.k_ts, p.k_hs) && ok(p.v, p.v_ls, p.v_ts, p.v_hs);
+// wide accesses need every row to start on such a boundary
+static int rows_vec(const Kv4Rows &p) {
+  for (int bytes : {32, 16}) {
+    const size_t u = bytes / (p.fp32 ? 4 : 2);   // elements
+    auto ok = [&](const void *x, size_t ls, size_t ts, size_t hs) { return (uintptr_t)x % bytes == 0 && ls % u == 0 && ts % u == 0 && hs % u == 0; };
+    if (ok(p.k, p.k_ls, p.k_ts, p.k_hs) && ok(p.v, p.v_ls, p.v_ts, p.v_hs)) return bytes;
+  }
+  return 0;
 }
 
 static int log2_of(int page) { return 31 - __builtin_clz((unsigned)page); }
@@ -31,12 +34,15 @@ static int log2_of(int page) { return 31 - __builtin_clz((unsigned)page); }
 template <bool WRITE>
 static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
   if (p.n < 1) return cudaSuccess;
-  // heads of a block: one while there are few blocks (a decode step's tokens: latency counts), several when there are many, so
-  // that the slot is looked up once and the next head's loads follow
+  // Heads of a block: one while there are few blocks (a decode step's tokens: latency counts), several when there are many, so
+  // that the slot is looked up once and the next head's loads follow.  Reading stores 512 bytes a row and pass (131072 tokens x 8
+  // heads of 128, bf16: 1 / 2 / 4 / 8 heads 138 / 110 / 115 / 122 us); writing, which computes more, gains up to 8 (271 / 221 /
+  // 202 / 192 us).
   const int64_t tg = ((int64_t)p.n + kKv4Block - 1) / kKv4Block;
-  const int hpb = tg * p.H * p.nl < 4096 ? 1 : 4;
+  int hpb = WRITE ? 8 : std::max(1, 512 / (p.hd * (p.fp32 ? 4 : 2)));
+  while (hpb > 1 && tg * ((p.H + hpb - 1) / hpb) * p.nl < 2048) hpb /= 2;
   const dim3 grid((unsigned)(tg * ((p.H + hpb - 1) / hpb)), p.nl);
-  const bool vec = rows_vec(p);
+  const int vec = rows_vec(p);
   const int sh = log2_of(p.page);
 #define KV4_ROWS(T, HD)                                                                 \
   do {                                                                                  \
@@ -139,7 +145,7 @@ cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
   p.nch_max = std::max(1, chunks_max(a.B, a.Hkv, a.max_len));
   p.qk_scale = a.scale * 1.4426950408889634f;
   const size_t u = a.fp32 ? 4 : 8;
-  p.vec = (uintptr_t)a.q % 16 == 0 && a.q_ls % u == 0 && a.q_ts % u == 0 && a.q_hs % u == 0;
+  p.vec = (uintptr_t)a.q % 16 == 0 && a.q_ls % u == 0 && a.q_ts % u == 0 && a.q_hs % u == 0 ? 16 : 0;
   // rows that a sequence brings to a key/value head, on average: the smallest tile that holds them
   const int64_t rows = ((int64_t)a.n_rows * p.G + a.B - 1) / a.B;
   const int tile = a.tile ? a.tile : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;

@@ -148,9 +148,10 @@ static __global__ void __launch_bounds__(kPlanThreads) k_kv4_plan(Kv4Plan p) {
 // c = round-half-even((x - m) / s) in 0..15 (0 where s = 0).  A group that holds a NaN or an infinity, or whose s or m leaves
 // bf16's range, is stored with s = m = NaN: what reads it sees NaN instead of a silently wrong number.
 // A thread holds 16 features of a key row and the same of the value row; 4 threads share a group, so the reductions take two
-// exchanges and a division serves 16 elements.  Rounding and packing run on the multiply-add pipe: x / s + 1.5 * 2^23 has
-// the code in its low bits, and eight of them are added up shifted.  A block covers 16 consecutive tokens of one or more
-// heads, so the rows of a storage block are written together.  Bound by HBM and instruction issue about equally.
+// exchanges and a division serves 16 elements.  The rest runs on the multiply-add pipe: quotient, rounding (by adding
+// 1.5 * 2^23) and packing (four codes are a number below 2^16); bf16 minima and maxima are taken two at a time.  A block
+// covers 16 consecutive tokens of one or more heads, so the rows of a storage block are written together.
+// Bound by HBM and instruction issue about equally.
 __device__ __forceinline__ float min_nan(float a, float b) {   // NaN if either is (fminf would drop it)
   float r;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -168,11 +169,27 @@ __device__ __forceinline__ float diff_err(float a, float b, float d) {
   return __fsub_rn(__fsub_rn(a, __fsub_rn(d, bb)), __fadd_rn(b, bb));
 }
 
+// 32 bytes in one access (32-byte aligned): whole sectors where a thread owns 32 bytes of a row
+__device__ __forceinline__ void ldg32(const void *p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+__device__ __forceinline__ void stg32(void *p, const float (&x)[8]) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+               : "memory");
+}
+
+// vec: bytes that every row is aligned to and may be accessed by at a time (32, 16, or 0: element by element)
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, float (&x)[8]);
+__device__ __forceinline__ void load8(const T *p, int vec, float (&x)[8]);
 template <>
-__device__ __forceinline__ void load8<float>(const float *p, bool vec, float (&x)[8]) {
-  if (vec) {
+__device__ __forceinline__ void load8<float>(const float *p, int vec, float (&x)[8]) {
+  if (vec == 32) {
+    uint32_t w[8];
+    ldg32(p, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+  } else if (vec) {
     const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   } else {
@@ -181,7 +198,7 @@ __device__ __forceinline__ void load8<float>(const float *p, bool vec, float (&x
   }
 }
 template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, bool vec, float (&x)[8]) {
+__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, int vec, float (&x)[8]) {
   if (vec) {
     const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -202,10 +219,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T *p, bool vec, const float (&x)[8]);
+__device__ __forceinline__ void store8(T *p, int vec, const float (&x)[8]);
 template <>
-__device__ __forceinline__ void store8<float>(float *p, bool vec, const float (&x)[8]) {
-  if (vec) {
+__device__ __forceinline__ void store8<float>(float *p, int vec, const float (&x)[8]) {
+  if (vec == 32) {
+    stg32(p, x);
+  } else if (vec) {
     reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
@@ -214,7 +233,7 @@ __device__ __forceinline__ void store8<float>(float *p, bool vec, const float (&
   }
 }
 template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, bool vec, const float (&x)[8]) {
+__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, int vec, const float (&x)[8]) {
   if (vec) {
     *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
   } else {
@@ -223,64 +242,185 @@ __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, bool vec
   }
 }
 
-// Codes of 16 features of a group whose 64 lie in 4 consecutive lanes (all 32 lanes call).  src: where x came from.
-// par = (s, m) as bf16 bits.
+constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: its unit is 1
+
+// a / s to the last place, and exactly where the quotient is a number of fp32 (inv = 1 / s to the last place)
+__device__ __forceinline__ float quotient(float a, float s, float inv) {
+  const float q = __fmul_rn(a, inv);
+  return fmaf(fmaf(-q, s, a), inv, q);
+}
+
+// The code of one element by exact comparisons: whatever the first guess, the remainder a - c s (which has no rounding error near
+// the guess) and the error of a = x - m decide; a tie goes to the even code.
+__device__ __forceinline__ uint32_t code_exact(float x, float s, float m) {
+  const float a = __fsub_rn(x, m), e = diff_err(x, m, a), half = 0.5f * s;
+  float c = rintf(fminf(fmaxf(__fdiv_rn(a, s), -1.f), 16.f));
+  const float d = fmaf(-c, s, a);
+  const bool odd = ((int)c & 1) != 0;
+  if (d > half || (d == half && (e > 0.f || (e == 0.f && odd)))) c += 1.f;
+  else if (d < -half || (d == -half && (e < 0.f || (e == 0.f && odd)))) c -= 1.f;
+  return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+}
+
+// 16 features as they were loaded, with their minimum and maximum
 template <typename T>
-__device__ __forceinline__ void quantise16(const float (&x)[2][8], const T *src, uint32_t (&word)[2], uint32_t &par) {
-  float lo = x[0][0], hi = x[0][0];
+struct Raw16;
+template <>
+struct Raw16<float> {
+  float v[16];
+  __device__ __forceinline__ void load(const float *p, int vec, bool live) {
+    if (live) {
+      float a[8], b[8];
+      load8<float>(p, vec, a); load8<float>(p + 8, vec, b);
 #pragma unroll
-  for (int i = 1; i < 16; ++i) { lo = min_nan(lo, x[i >> 3][i & 7]); hi = max_nan(hi, x[i >> 3][i & 7]); }
+      for (int i = 0; i < 8; ++i) { v[i] = a[i]; v[8 + i] = b[i]; }
+    } else {
 #pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      for (int i = 0; i < 16; ++i) v[i] = 0.f;
+    }
   }
+  __device__ __forceinline__ float get(int i) const { return v[i]; }
+  __device__ __forceinline__ void range(float &lo, float &hi) const {
+    lo = hi = v[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) { lo = min_nan(lo, v[i]); hi = max_nan(hi, v[i]); }
+  }
+};
+template <>
+struct Raw16<__nv_bfloat16> {
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const __nv_bfloat16 *p, int vec, bool live) {
+    if (live && vec == 32) {
+      ldg32(p, w);
+    } else if (live && vec) {
+      const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p)), b = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        w[i] = live ? (uint32_t)__bfloat16_as_ushort(p[2 * i]) | (uint32_t)__bfloat16_as_ushort(p[2 * i + 1]) << 16 : 0u;
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ void range(float &lo, float &hi) const {
+    uint32_t a = w[0], b = w[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(w[i]));
+      asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(b), "r"(w[i]));
+    }
+    lo = min_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    hi = max_nan(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u));
+  }
+};
+
+// What a group's codes are computed with: scale, low, 1 / scale, and how.
+enum { KV4_Q_NAN = 1, KV4_Q_ZERO = 2, KV4_Q_EXACT = 4, KV4_Q_BORDER = 8 };
+struct Quant4 {
+  float s, m, inv;
+  uint32_t how;   // 0: fast
+};
+template <typename T>
+__device__ __forceinline__ Quant4 quant4(float lo, float hi) {
+  Quant4 q;
   const float r = __fsub_rn(hi, lo);
   // r / 15 in fp32 is the rounding of the true quotient wherever hi - lo has no error of its own; else through fp64
   float quo = __fdiv_rn(r, 15.f);
   if (diff_err(hi, lo, r) != 0.f) quo = (float)(((double)hi - (double)lo) / 15.0);
-  const float s = __bfloat162float(__float2bfloat16_rn(quo)), m = __bfloat162float(__float2bfloat16_rn(lo));
+  q.s = __bfloat162float(__float2bfloat16_rn(quo));
+  q.m = __bfloat162float(__float2bfloat16_rn(lo));
+  q.inv = __fdividef(1.f, q.s);
+  // Fast: no code leaves 0..15 (the quotient is monotonous: its ends tell), 1 / s is a number, and for bf16 additionally
+  // every x - m near the border of two codes is exact.  The latter fails only where m lies 2^16 below x, or x that far below
+  // an m that lies on a border itself: elsewhere a quotient that is not a tie is further from one than fp32 can blur.
+  const float c_lo = __fsub_rn(__fadd_rn(quotient(__fsub_rn(lo, q.m), q.s, q.inv), kMagic), kMagic);
+  const float c_hi = __fsub_rn(__fadd_rn(quotient(__fsub_rn(hi, q.m), q.s, q.inv), kMagic), kMagic);
+  bool fast = q.s >= 1e-30f && c_lo >= 0.f && c_hi <= 15.f;
+  q.how = 0u;
+  if (sizeof(T) == 2) {
+    const float q_m = quotient(-q.m, q.s, q.inv), c_m = __fsub_rn(__fadd_rn(q_m, kMagic), kMagic);
+    fast = fast && !(q.m != 0.f && fabsf(q.m) < q.s * 0.000244140625f);
+    if (fabsf(__fsub_rn(q_m, c_m)) == 0.5f) q.how = KV4_Q_BORDER;   // (one group in a hundred)
+  }
+  if (!fast) q.how |= KV4_Q_EXACT;
+  if (q.s == 0.f) q.how = KV4_Q_ZERO;
+  if (!(isfinite(q.s) && isfinite(q.m))) q.how = KV4_Q_NAN;
+  return q;
+}
+
+// Codes of 16 features with the group's q.  src: where x came from.  par = (s, m) as bf16 bits.
+template <typename T>
+__device__ __forceinline__ void encode16(const Raw16<T> &x, const T *src, const Quant4 &q, uint32_t (&word)[2], uint32_t &par) {
   word[0] = word[1] = 0u;
-  if (!(isfinite(s) && isfinite(m))) {
-    par = 0x7fc07fc0u;
-    return;
-  }
-  par = (__float_as_uint(s) >> 16) | (__float_as_uint(m) & 0xffff0000u);
-  if (s == 0.f) return;
-  constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: its unit is 1
-  const bool tiny = s < 1e-30f;          // 1/s may overflow
-  const float half = 0.5f * s, inv = tiny ? 0.f : __fdividef(1.f, s);
-  uint32_t check = 0u;
+  par = q.how & KV4_Q_NAN ? 0x7fc07fc0u : (__float_as_uint(q.s) >> 16) | (__float_as_uint(q.m) & 0xffff0000u);
+  if (q.how & (KV4_Q_NAN | KV4_Q_ZERO)) return;
+  const float s = q.s, m = q.m, inv = q.inv, half = 0.5f * s;
+  bool fast = !(q.how & KV4_Q_EXACT);
+  if (q.how & KV4_Q_BORDER) {
+    const float few = fabsf(m) * 0.00006103515625f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float a = __fsub_rn(x[i >> 3][i & 7], m);
-    float t = fmaf(a, inv, kMagic);
-    const float c = __fsub_rn(t, kMagic);
-    // a * inv may be off by a few units in the last place: codes whose exact remainder (a - c s has no rounding error here) is
-    // not below half a step are looked at again
-    if (!(fabsf(fmaf(-c, s, a)) < half)) check |= 1u << i;
-    t = fminf(fmaxf(t, kMagic), kMagic + 15.f);
-    word[i >> 3] += __float_as_uint(t) << (4 * (i & 7));
+    for (int i = 0; i < 16; ++i) fast = fast && (x.get(i) == 0.f || fabsf(x.get(i)) >= few);
   }
-  // the bits of 1.5 * 2^23 that were added up with the codes: 0x4b400000 shifted by 0, 4, .. 28 places
-  constexpr uint32_t kBias = 0x4b400000u + 0xb4000000u + 0x40000000u;
-  word[0] -= kBias;
-  word[1] -= kBias;
+  uint32_t check = 0u;   // elements to be looked at again
+  if (fast) {
+    float c[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float a = __fsub_rn(x.get(i), m);
+      if (sizeof(T) == 2) {
+        c[i] = __fsub_rn(__fadd_rn(quotient(a, s, inv), kMagic), kMagic);
+      } else {
+        // fp32: a guess, and the remainder tells where it may be wrong
+        c[i] = __fsub_rn(fmaf(a, inv, kMagic), kMagic);
+        if (!(fabsf(fmaf(-c[i], s, a)) < half)) check |= 1u << i;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float *y = c + 8 * k + 4 * i;
+        h[i] = __float_as_uint(__fadd_rn(fmaf(fmaf(fmaf(y[3], 16.f, y[2]), 16.f, y[1]), 16.f, y[0]), 8388608.f));
+      }
+      word[k] = __byte_perm(h[0], h[1], 0x5410);
+    }
+  } else {
+    check = 0xffffu;
+  }
   while (check) {
-    const int i = __ffs(check) - 1;
+    const int i = __ffs(check) - 1, at = 4 * (i & 7);
     check &= check - 1;
-    const float xi = to_f<T>(src[i]), a = __fsub_rn(xi, m);
-    float c = tiny ? rintf(fminf(fmaxf(__fdiv_rn(a, s), -1.f), 16.f)) : __fsub_rn(fmaf(a, inv, kMagic), kMagic);
-    // the exact remainder and the error of a decide; a tie goes to the even code
-    const float d = fmaf(-c, s, a), e = diff_err(xi, m, a);
-    const bool odd = ((int)c & 1) != 0;
-    if (d > half || (d == half && (e > 0.f || (e == 0.f && odd)))) c += 1.f;
-    else if (d < -half || (d == -half && (e < 0.f || (e == 0.f && odd)))) c -= 1.f;
-    const uint32_t code = (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
-    const int at = 4 * (i & 7);
+    const uint32_t code = code_exact(to_f<T>(src[i]), s, m);
     if (i < 8) word[0] = (word[0] & ~(15u << at)) | code << at;
     else word[1] = (word[1] & ~(15u << at)) | code << at;
   }
+}
+
+// Codes of 16 features of a key row and of the same value row; a group's 64 features lie in 4 consecutive lanes (all 32 lanes
+// call).  Of each pair of lanes one works out the keys' scale and the other the values', and they exchange them.
+template <typename T>
+__device__ __forceinline__ void quantise16(const Raw16<T> &xk, const Raw16<T> &xv, const T *ks, const T *vs, uint32_t (&wk)[2], uint32_t (&wv)[2],
+                                           uint32_t &pk, uint32_t &pv) {
+  float klo, khi, vlo, vhi;
+  xk.range(klo, khi);
+  xv.range(vlo, vhi);
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    klo = min_nan(klo, __shfl_xor_sync(0xffffffffu, klo, o));
+    khi = max_nan(khi, __shfl_xor_sync(0xffffffffu, khi, o));
+    vlo = min_nan(vlo, __shfl_xor_sync(0xffffffffu, vlo, o));
+    vhi = max_nan(vhi, __shfl_xor_sync(0xffffffffu, vhi, o));
+  }
+  const bool odd = threadIdx.x & 1;
+  const Quant4 mine = quant4<T>(odd ? vlo : klo, odd ? vhi : khi);
+  Quant4 other;
+  other.s = __shfl_xor_sync(0xffffffffu, mine.s, 1);
+  other.m = __shfl_xor_sync(0xffffffffu, mine.m, 1);
+  other.inv = __shfl_xor_sync(0xffffffffu, mine.inv, 1);
+  other.how = __shfl_xor_sync(0xffffffffu, mine.how, 1);
+  encode16<T>(xk, ks, odd ? other : mine, wk, pk);
+  encode16<T>(xv, vs, odd ? mine : other, wv, pv);
 }
 
 // address of the storage block and place in it of a slot, for head 0 (head h: h * page / 16 blocks further); page = 2^page_sh
@@ -300,7 +440,7 @@ constexpr int kReadThreads = kKv4Block * 8;
 
 // grid (16-token groups x head groups of `hpb` heads, layers)
 template <typename T, int HD>
-static __global__ void __launch_bounds__(kWriteThreads(HD)) k_kv4_write(Kv4Rows p, bool vec, int hpb, int page_sh) {
+static __global__ void __launch_bounds__(kWriteThreads(HD)) k_kv4_write(Kv4Rows p, int vec, int hpb, int page_sh) {
   typedef Kv4Fmt<HD> F;
   constexpr int LPR = HD / 16;
   const int j = threadIdx.x % LPR, hg = (p.H + hpb - 1) / hpb, l = blockIdx.y;
@@ -313,17 +453,19 @@ static __global__ void __launch_bounds__(kWriteThreads(HD)) k_kv4_write(Kv4Rows 
   const Place4 at = place4(p, l, live ? slot : 0, page_sh, F::kBytes);
   const size_t head_bytes = (size_t)(p.page / kKv4Block) * F::kBytes;
   const int grp = j / 4, r = j % 4;   // group of this thread's features, place in it
+  Raw16<T> nk, nv;                    // the next head's rows, on their way while the current ones are worked on
+  nk.load(k + (size_t)h0 * p.k_hs, vec, live);
+  nv.load(v + (size_t)h0 * p.v_hs, vec, live);
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
-    float xk[2][8] = {}, xv[2][8] = {};
+    const Raw16<T> xk = nk, xv = nv;
     const T *ks = k + (size_t)h * p.k_hs, *vs = v + (size_t)h * p.v_hs;
-    if (live) {
-      load8<T>(ks, vec, xk[0]); load8<T>(ks + 8, vec, xk[1]);
-      load8<T>(vs, vec, xv[0]); load8<T>(vs + 8, vec, xv[1]);
+    if (h + 1 < h1) {
+      nk.load(ks + p.k_hs, vec, live);
+      nv.load(vs + p.v_hs, vec, live);
     }
     uint32_t pk, pv, wk[2], wv[2];
-    quantise16<T>(xk, ks, wk, pk);
-    quantise16<T>(xv, vs, wv, pv);
+    quantise16<T>(xk, xv, ks, vs, wk, wv, pk, pv);
     if (live) {
       uint8_t *blk = at.blk + h * head_bytes;
       // key words 2r, 2r + 1 of a group lie side by side; value words at (2r) NG + grp, (2r + 1) NG + grp
@@ -349,7 +491,7 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t par, float (&x)[8])
 }
 
 template <typename T, int HD>
-static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, bool vec, int hpb, int page_sh) {
+static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, int vec, int hpb, int page_sh) {
   typedef Kv4Fmt<HD> F;
   constexpr int NG = F::NG, UN = 2;
   const int j = threadIdx.x % 8, hg = (p.H + hpb - 1) / hpb, l = blockIdx.y;
@@ -467,7 +609,7 @@ struct Attn4Params {
   Kv4Attn a;
   int G, chunk, nch_max;
   float qk_scale;   // softmax scale * log2(e)
-  bool vec;         // q may be read 16 bytes at a time
+  int vec;          // q may be read 16 bytes at a time (16) or not (0)
 };
 
 __device__ __forceinline__ float ex2(float x) {
