@@ -60,13 +60,18 @@ static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
 cudaError_t kv4_write(const Kv4Rows &p, cudaStream_t st) { return rows_launch<true>(p, st); }
 cudaError_t kv4_read(const Kv4Rows &p, cudaStream_t st) { return rows_launch<false>(p, st); }
 
-// Keys of a split.  It depends on the number of (sequence, key/value head) pairs only, as in the attention over the
-// unquantised cache: not on lengths, query rows or layers, so that every call merges a row's keys in the same order.
-int kv4_chunk(int pairs) { return pairs < 32 ? 256 : pairs < 256 ? 512 : 1024; }
+// Keys of a split, as a power of two: it depends on the number of (sequence, key/value head) pairs and the longest length allowed
+// only -- not on the lengths, query rows or layers of a call -- so that calls on one cache merge a row's keys in the same order.
+// Few pairs: short splits, many warps; many pairs: long ones, which cost less to begin and to end; and at most 256 of them.
+static int chunk_shift(int pairs, int max_len) {
+  int sh = pairs < 32 ? 7 : pairs < 256 ? 8 : 9;
+  while (((int64_t)max_len >> sh) > 256 && sh < 11) ++sh;
+  return sh;
+}
 
 static int chunks_max(int B, int Hkv, int max_len) {
-  const int c = kv4_chunk(B * Hkv);
-  return (int)(((int64_t)max_len + c - 1) / c);
+  const int sh = chunk_shift(B * Hkv, max_len);
+  return (int)(((int64_t)max_len + (1 << sh) - 1) >> sh);
 }
 
 int kv4_attention_launches(int B, int Hkv, int max_len) { return chunks_max(B, Hkv, max_len) > 1 ? 2 : 1; }
@@ -117,7 +122,7 @@ static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) 
   k_kv4_attn<T, HD, RW, NT><<<grid, kAttn4Threads, smem, st>>>(p);
   if (p.nch_max > 1) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.n_rows * a.Hq, a.nl); cfg.blockDim = dim3(128); cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)a.n_rows * a.Hq, a.nl); cfg.blockDim = dim3(32 * kMergeWarps); cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // scheduled while the splits finish, waits for their results
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -141,7 +146,7 @@ cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
   Attn4Params p{};
   p.a = a;
   p.G = a.Hq / a.Hkv;
-  p.chunk = kv4_chunk(a.B * a.Hkv);
+  p.chunk_sh = chunk_shift(a.B * a.Hkv, a.max_len);
   p.nch_max = std::max(1, chunks_max(a.B, a.Hkv, a.max_len));
   p.qk_scale = a.scale * 1.4426950408889634f;
   const size_t u = a.fp32 ? 4 : 8;
@@ -301,7 +306,7 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   if (need > 0 && (!workspace || workspace_bytes < need)) return refuse(SNLP_ERR_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : (size_t)0, need);
   if ((uintptr_t)workspace % 16) return refuse(SNLP_ERR_ARG, "%s: the workspace must be 16-byte aligned", who);
   const int64_t G = args->n_head / pool->n_kv_head;
-  const int64_t units = (args->n_rows * G / 2 + args->B) * (int64_t)(((int64_t)a.max_len + 255) / 256);
+  const int64_t units = (args->n_rows * G / 2 + args->B) * (int64_t)(((int64_t)a.max_len + 127) / 128);
   if (units > 0x7fffffffLL || (int64_t)args->n_rows * args->n_head > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
   if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
   int dev = 0, n_sm = 0;

@@ -565,25 +565,27 @@ static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, int
 // probability times its scale) is split into a multiple of 16 (11 bits on one grid for the whole row: the products with
 // codes are whole numbers and their sums exact) and an fp16 remainder with an accumulator of its own, 22 bits in all, and
 // the second product's sums over a block's keys are added to the running output by fp32 additions, which round.
-// Work.  A unit is (layer, key/value head, sequence, tile of RW NT query rows, chunk of keys); a thread block of four warps
-// takes a contiguous range of the list of all units (its place in it comes from a prefix sum over the lengths), each warp
-// every fourth stage of a unit, through its own ring of cp.async stages that runs on across units.  The block joins its
-// warps' columns in a fixed order; rows with several chunks are joined by k_kv4_merge in chunk order.  Chunk boundaries
-// depend on the number of (sequence, head) pairs only and a row's arithmetic on its own visible keys and RW, so for one RW a
-// row comes out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
+// Work.  A unit is (layer, key/value head, sequence, tile of RW NT query rows, chunk of keys) and belongs to one warp, which walks
+// it in stages of 16 KB keys.  A thread block has a contiguous range of the list of all units (its place in it comes from a
+// prefix sum over the lengths), of which its four warps take the next one as they come (dealt out beforehand, the warps with
+// a unit more than others ran alone at the end: 94 us for the last of 160 x 10 heads x 2048 keys where the median was 76), each
+// with a ring of cp.async stages of its own that runs on across units: after the prefix sum no warp waits for another.  A
+// warp joins its columns at the end of a unit; rows with several chunks are joined by k_kv4_merge in chunk order.  The chunk length depends on the number of (sequence, head) pairs and the longest length allowed,
+// and a row's arithmetic on its own visible keys and RW, so for one RW a row comes out the same whether it is decoded alone,
+// in a verify block or in a sweep over all layers.
 // Bound: HBM for few rows (hd 128: 144 bytes a key and head), instruction issue and the mma.sync rate beyond.
 constexpr int kAttn4Warps = 4, kAttn4Threads = 32 * kAttn4Warps;
-constexpr int kAttn4Batch = 16;   // units whose descriptions are in shared memory at a time
 
 // One unit of the list
 struct Unit4 {
   int b, h, l;          // sequence, key/value head, layer
   int r0, nrows;        // first row of the tile within the sequence's T * G rows, rows in it
-  int k0, kend;         // keys of this unit: k0 .. kend-1 (empty: kend <= k0)
-  int c, nch;           // chunk, chunks that the tile's rows can see
+  int k0, kend;         // keys of this unit: k0 .. kend-1 (none: kend <= k0)
   int tok0, ahead, cap; // first row of the sequence; row i sees keys 0 .. ahead + i, cut to cap keys
-  int vis0, vis1;       // keys that the tile's first and last row see
+  int flags;
 };
+enum { UNIT4_LIVE = 1, UNIT4_WHOLE = 2, UNIT4_SAME = 4, UNIT4_ONE = 8 };   // leaves something behind; its rows see one chunk; ... all the same keys; ... are of one token
+constexpr int kUnitBatch = 32;   // units of a block that are described in shared memory at a time
 
 template <typename T, int HD, int RW, int NT>
 struct Attn4Cfg {
@@ -597,17 +599,16 @@ struct Attn4Cfg {
   __host__ __device__ static constexpr int block_at(int j) { return j * Kv4Fmt<HD>::kBytes + (SUB == 1 ? 0 : HD == 128 ? (j & 1) * 16 + (j >> 1) * 64 : j * 32); }
   static constexpr int kStage = block_at(KB - 1) + Kv4Fmt<HD>::kBytes;
   static constexpr int kRing = kAttn4Warps * kRingLen * kStage;
-  static constexpr int kOutLd = HD + 4;                              // a column's outputs, then its maximum and denominator
-  static constexpr bool kOutInRing = 8 * kOutLd * 4 * NT <= kStage;  // a warp's results fit the stage that it has read last
-  static constexpr int kOut = kOutInRing ? 0 : kAttn4Warps * 8 * NT * kOutLd * 4;
-  static constexpr int kFixed = kRing + kOut + kAttn4Batch * (int)sizeof(Unit4);   // + (B + 1) ints
+  static constexpr int kOutLd = HD + 4;         // a column's outputs, then its maximum and denominator
+  static_assert(8 * kOutLd * 4 <= kStage, "eight columns fit the stage that a warp has read last");
+  static constexpr int kFixed = kRing + kUnitBatch * (int)sizeof(Unit4);   // + (B + 1) ints
   // blocks of an SM: three fit the shared memory; what needs more than 168 registers runs two
   static constexpr int kResident = NT == 1 && sizeof(T) == 2 ? 3 : 2;
 };
 
 struct Attn4Params {
   Kv4Attn a;
-  int G, chunk, nch_max;
+  int G, chunk_sh, nch_max;   // chunks of 2^chunk_sh keys
   float qk_scale;   // softmax scale * log2(e)
   int vec;          // q may be read 16 bytes at a time (16) or not (0)
 };
@@ -661,22 +662,23 @@ __device__ __forceinline__ Seq4 seq4(const Kv4Attn &a, int b) {
 }
 __device__ __forceinline__ int seq4_visible(int ahead, int cap, int i) { return min(max(ahead + i + 1, 0), cap); }   // keys that row i sees
 
+__device__ __forceinline__ int chunks4(const Attn4Params &p, int keys) { return max((keys + (1 << p.chunk_sh) - 1) >> p.chunk_sh, 1); }
+
 __device__ __forceinline__ Unit4 unit4(const Attn4Params &p, const int *uoff, int tile, int x, int y) {
   Unit4 u;
   u.b = find_seq(uoff, p.a.B, x);
-  const Seq4 s = seq4(p.a, u.b);
   u.h = y % p.a.Hkv;
   u.l = y / p.a.Hkv;
-  const int nchb = max((s.cap + p.chunk - 1) / p.chunk, 1), w = x - uoff[u.b];
-  u.c = w % nchb;
+  const Seq4 s = seq4(p.a, u.b);
+  const int nchb = chunks4(p, s.cap), w = x - uoff[u.b];
   u.r0 = (w / nchb) * tile;
   u.nrows = min(s.T * p.G - u.r0, tile);
   u.tok0 = s.row0; u.ahead = s.len - s.T; u.cap = s.cap;
-  u.vis0 = seq4_visible(u.ahead, u.cap, u.r0 / p.G);
-  u.vis1 = seq4_visible(u.ahead, u.cap, (u.r0 + u.nrows - 1) / p.G);
-  u.nch = max((u.vis1 + p.chunk - 1) / p.chunk, 1);
-  u.k0 = u.c * p.chunk;
-  u.kend = min(u.k0 + p.chunk, u.vis1);
+  // keys of the first and last row
+  const int vis0 = seq4_visible(u.ahead, u.cap, s.T == 1 ? 0 : u.r0 / p.G), vis1 = seq4_visible(u.ahead, u.cap, s.T == 1 ? 0 : (u.r0 + u.nrows - 1) / p.G);
+  u.k0 = (w % nchb) << p.chunk_sh;
+  u.kend = min(u.k0 + (1 << p.chunk_sh), vis1);
+  u.flags = (u.k0 == 0 || u.k0 < vis1 ? UNIT4_LIVE : 0) | (vis1 <= 1 << p.chunk_sh ? UNIT4_WHOLE : 0) | (vis0 == vis1 ? UNIT4_SAME : 0) | (s.T == 1 ? UNIT4_ONE : 0);
   return u;
 }
 
@@ -725,12 +727,12 @@ static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>
   constexpr float kLow = CEN ? 1.f : 16777216.f, kHigh = CEN ? 1.f : 1048576.f;   // what a product with a low / high code is multiplied by
   constexpr float kHighQ = kLow == kHigh ? 1.f : 0.0625f;                         // query elements that meet high codes
   extern __shared__ __align__(16) unsigned char attn4_sm[];
-  __shared__ int s_tmp[kAttn4Warps];                      // scan totals; later, where each warp left its results
+  __shared__ int s_tmp[kAttn4Warps], s_next;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int ka = (g & 1) * 4 + (g >> 1);                  // kappa(g): this lane's score rows are keys ka and ka + 8 of a block
   const int sub = 2 * t / RW;                             // whose block of a set this lane's columns 2t, 2t + 1 stand for
   unsigned char *ring = attn4_sm + warp * S::kRingLen * S::kStage;
-  Unit4 *units = reinterpret_cast<Unit4 *>(attn4_sm + S::kRing + S::kOut);
+  Unit4 *units = reinterpret_cast<Unit4 *>(attn4_sm + S::kRing);
   int *uoff = reinterpret_cast<int *>(attn4_sm + S::kFixed);
   const Kv4Attn &a = p.a;
   pdl_wait();
@@ -743,7 +745,7 @@ static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>
       int n = 0;
       if (b < a.B) {
         const Seq4 s = seq4(a, b);
-        n = ((s.T * p.G + kTile - 1) / kTile) * max((s.cap + p.chunk - 1) / p.chunk, 1);
+        n = ((s.T * p.G + kTile - 1) / kTile) * chunks4(p, s.cap);
       }
       int v = n;
 #pragma unroll
@@ -768,7 +770,6 @@ static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>
   const int U = uoff[a.B];
   const long long total = (long long)U * a.Hkv * a.nl;
   const long long u0 = total * blockIdx.x / gridDim.x, u1 = total * (blockIdx.x + 1) / gridDim.x;
-  if (u0 >= u1) return;
 
   const int bpp = a.page / kKv4Block, page_sh = 31 - __clz(a.page);
   const bool whole = a.page >= S::kKeys;   // a stage lies within a page
@@ -777,480 +778,516 @@ static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>
   uint32_t qf[NT][NSP][NG * KS][2];
   float qfac[NT][2], qsum[NT][2][NG];      // of this lane's two columns: power-of-two factor with the scale, scaled feature sums
 
-  for (long long first = u0; first < u1; first += kAttn4Batch) {
-    const int nu = (int)min(u1 - first, (long long)kAttn4Batch);
-    if (first != u0) __syncthreads();      // every warp is done with the batch before
-    if (tid < nu) units[tid] = unit4(p, uoff, kTile, (int)((first + tid) % U), (int)((first + tid) / U));
-    __syncthreads();
+  int slot_w = 0, slot_r = 0, issued = 0, done = 0;   // ring places to be filled and read next; stages requested and read
 
-    // ---- copy side: this warp's stages in order, kRingLen - 1 of them ahead of the arithmetic ----
-    int pu = 0, pi = 0, pn = 0, pk0 = 0, ent = -1, slot_w = 0;
-    const uint8_t *pbase = nullptr;        // the unit's layer and head within page 0
-    auto enter = [&]() {                   // stages of unit pu, and the page of each of their blocks (lane KB i + j: block j of stage i)
-      const Unit4 &u = units[pu];
-      const int kend = u.kend;
+  for (long long first = u0; first < u1; first += kUnitBatch) {
+  const int nu = (int)min(u1 - first, (long long)kUnitBatch);
+  if (first != u0) __syncthreads();        // every warp is done with the batch before
+  if (tid < nu) {
+    const unsigned long long v = (unsigned long long)(first + tid);
+    const int y = v >> 32 ? (int)(v / (unsigned)U) : (int)((unsigned)v / (unsigned)U);   // (a 32-bit division where it will do)
+    units[tid] = unit4(p, uoff, kTile, (int)(v - (unsigned long long)y * (unsigned)U), y);
+  }
+  if (tid == 0) s_next = 0;
+  __syncthreads();
+
+  // units that this warp has taken and not finished, eight bits each, the one in work lowest; how many, and of how many the
+  // copies have begun
+  uint32_t queue = 0u;
+  int taken = 0, entered = 0;
+  bool more = true;
+  auto take = [&]() {                      // the block's next unit
+    int i = 0;
+    if (lane == 0) i = atomicAdd(&s_next, 1);
+    i = __shfl_sync(0xffffffffu, i, 0);
+    more = i < nu;
+    if (more) queue |= (uint32_t)i << (8 * taken++);
+    return more;
+  };
+
+  // ---- copy side: this warp's stages in order, kRingLen - 1 of them ahead of the arithmetic ----
+  int pi = 0, pn = 0, pk0 = 0, ent = -1, pid = 0;
+  const uint8_t *pbase = nullptr;          // the unit's layer and head within page 0
+  auto copy_next = [&]() {                 // request the next stage; false: there is none (yet)
+    while (pi >= pn) {
+      if (entered >= taken && (!more || taken == 4 || !take())) return false;
+      pid = queue >> (8 * entered++) & 255u;
+      const Unit4 &u = units[pid];
       pk0 = u.k0; pi = 0;
-      const int ns = (max(kend - pk0, 0) + S::kKeys - 1) / S::kKeys;
-      pn = (ns - warp + kAttn4Warps - 1) / kAttn4Warps;
+      pn = (max(u.kend - pk0, 0) + S::kKeys - 1) / S::kKeys;
       pbase = a.pool + (size_t)u.l * a.pool_ls + (size_t)u.h * bpp * F::kBytes;
-      ent = -1;
-      const int key = pk0 + ((lane / KB) * kAttn4Warps + warp) * S::kKeys + (lane % KB) * kKv4Block;
-      if (lane / KB < pn && key < kend) ent = a.table[(size_t)u.b * a.tstride + (key >> page_sh)];
-    };
-    enter();
-    auto copy_next = [&]() {               // request the next stage (if any); always closes a group
-      while (pi >= pn && pu < nu)
-        if (++pu < nu) enter();
-      if (pu < nu) {
-        constexpr int NC = F::kBytes / 16;   // 16-byte pieces of a block; piece c = lane + 32 i of the stage
-        unsigned char *dst = ring + slot_w * S::kStage + lane * 16;
-        const int key = pk0 + (pi * kAttn4Warps + warp) * S::kKeys;
-        const uint8_t *src[KB];
-        bool ok[KB];
-        if (whole) {                         // one page: what follows the last key is copied too and masked with it
-          const int e = __shfl_sync(0xffffffffu, ent, KB * pi);
-          ok[0] = (unsigned)e < (unsigned)a.n_pages;
-          src[0] = pbase + (ok[0] ? (size_t)e * page_bytes : 0) + (key & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16;
-#pragma unroll
-          for (int j = 1; j < KB; ++j) { ok[j] = ok[0]; src[j] = src[0]; }
-        } else
-#pragma unroll
-        for (int j = 0; j < KB; ++j) {
-          const int e = __shfl_sync(0xffffffffu, ent, KB * pi + j);
-          ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
-          src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + ((key + 16 * j) & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16 - j * F::kBytes;
-        }
-#pragma unroll
-        for (int i = 0; i < (KB * NC + 31) / 32; ++i) {
-          constexpr int last = KB - 1;
-          const int j0 = 32 * i / NC, j1 = (32 * i + 31) / NC < last ? (32 * i + 31) / NC : last;
-          const bool up = j1 > j0 && lane >= j1 * NC - 32 * i;
-          if (32 * i + 31 < KB * NC || lane < KB * NC - 32 * i)
-            cp_async16(dst + 512 * i + (up ? S::block_at(j1) - j1 * F::kBytes : S::block_at(j0) - j0 * F::kBytes), (up ? src[j1] : src[j0]) + 512 * i,
-                       up ? ok[j1] : ok[j0]);
-        }
-        ++pi;
-        slot_w = slot_w + 1 == S::kRingLen ? 0 : slot_w + 1;
+      // its queries on their way to the first-level cache: a lane the row of its column, a line of 128 bytes each of four lanes
+      const int r = g % RW;
+      if (r < u.nrows && t * 128 < HD * (int)sizeof(T)) {
+        const int ri = u.r0 + r, i = u.flags & UNIT4_ONE ? 0 : ri / p.G, hq = u.h * p.G + ri - i * p.G;
+        const T *src = (const T *)a.q + (size_t)u.l * a.q_ls + (size_t)(u.tok0 + i) * a.q_ts + (size_t)hq * a.q_hs;
+        asm volatile("prefetch.global.L1 [%0];" ::"l"((const char *)src + t * 128));
       }
-      cp_async_commit();
-    };
+    }
+    if (KB * pi % 32 == 0) {               // the pages of the next 32 blocks, one a lane
+      const Unit4 &u = units[pid];
+      const int key = pk0 + (KB * pi + lane) * kKv4Block;
+      ent = key < u.kend ? a.table[(size_t)u.b * a.tstride + (key >> page_sh)] : -1;
+    }
+    constexpr int NC = F::kBytes / 16;     // 16-byte pieces of a block; piece c = lane + 32 i of the stage
+    unsigned char *dst = ring + slot_w * S::kStage + lane * 16;
+    const int key = pk0 + pi * S::kKeys;
+    const uint8_t *src[KB];
+    bool ok[KB];
+    if (whole) {                           // one page: what follows the last key is copied too and masked with it
+      const int e = __shfl_sync(0xffffffffu, ent, KB * pi % 32);
+      ok[0] = (unsigned)e < (unsigned)a.n_pages;   // no such page: zeros
+      src[0] = pbase + (ok[0] ? (size_t)e * page_bytes : 0) + (key & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16;
 #pragma unroll
-    for (int i = 0; i < S::kRingLen - 1; ++i) copy_next();
+      for (int j = 1; j < KB; ++j) { ok[j] = ok[0]; src[j] = src[0]; }
+    } else {
+#pragma unroll
+      for (int j = 0; j < KB; ++j) {
+        const int e = __shfl_sync(0xffffffffu, ent, (KB * pi + j) % 32);
+        ok[j] = (unsigned)e < (unsigned)a.n_pages;   // absent block (past the end, or no such page): zeros
+        src[j] = pbase + (ok[j] ? (size_t)e * page_bytes : 0) + ((key + 16 * j) & (a.page - 1)) / kKv4Block * F::kBytes + lane * 16 - j * F::kBytes;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < (KB * NC + 31) / 32; ++i) {
+      constexpr int last = KB - 1;
+      const int j0 = 32 * i / NC, j1 = (32 * i + 31) / NC < last ? (32 * i + 31) / NC : last;
+      const bool up = j1 > j0 && lane >= j1 * NC - 32 * i;
+      if (32 * i + 31 < KB * NC || lane < KB * NC - 32 * i)
+        cp_async16(dst + 512 * i + (up ? S::block_at(j1) - j1 * F::kBytes : S::block_at(j0) - j0 * F::kBytes), (up ? src[j1] : src[j0]) + 512 * i,
+                   up ? ok[j1] : ok[j0]);
+    }
+    cp_async_commit();
+    ++pi; ++issued;
+    slot_w = slot_w + 1 == S::kRingLen ? 0 : slot_w + 1;
+    return true;
+  };
+  while (issued < done + S::kRingLen - 1 && copy_next()) {}
 
-    // ---- arithmetic ----
-    int slot_r = 0;
-    for (int cu = 0; cu < nu; ++cu) {
-      const Unit4 u = units[cu];
-      if (u.b != q_b || u.l * a.Hkv + u.h != q_y || u.r0 != q_r0) {
-        q_b = u.b; q_y = u.l * a.Hkv + u.h; q_r0 = u.r0;
+  // ---- arithmetic ----
+  while (taken > 0 || (more && take())) {
+    const Unit4 u = units[queue & 255u];
+    auto finish = [&]() { queue >>= 8; --taken; entered = max(entered - 1, 0); };
+    if (!(u.flags & UNIT4_LIVE)) {   // (a chunk that no row of the tile sees)
+      finish();
+      continue;
+    }
+    const int ul = u.l, uh = u.h, uy = ul * a.Hkv + uh;
+    if (u.b != q_b || uy != q_y || u.r0 != q_r0) {
+      q_b = u.b; q_y = uy; q_r0 = u.r0;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int r = nt * 8 + g % RW;     // fragment column g: row r of the tile
-          float x[NG][16];
-          if (r < u.nrows) {
-            const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
-            const T *src = (const T *)a.q + (size_t)u.l * a.q_ls + (size_t)tok * a.q_ts + (size_t)hq * a.q_hs + 16 * t;
-#pragma unroll
-            for (int n = 0; n < NG; ++n) {
-              float y[8];
-              load8<T>(src + n * kKv4Group, p.vec, y);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[n][i] = y[i];
-              load8<T>(src + n * kKv4Group + 8, p.vec, y);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[n][8 + i] = y[i];
-            }
-          } else {
-#pragma unroll
-            for (int n = 0; n < NG; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
-          }
-          float top = 0.f, sum[NG];
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 8 + g % RW;     // fragment column g: row r of the tile
+        float x[NG][16];
+        if (r < u.nrows) {
+          const int ri = u.r0 + r, i1 = u.flags & UNIT4_ONE ? 0 : ri / p.G, tok = u.tok0 + i1, hq = uh * p.G + ri - i1 * p.G;
+          const T *src = (const T *)a.q + (size_t)ul * a.q_ls + (size_t)tok * a.q_ts + (size_t)hq * a.q_hs + 16 * t;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            sum[n] = 0.f;
+            float y[8];
+            load8<T>(src + n * kKv4Group, p.vec, y);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) { top = max_nan(top, fabsf(x[n][i])); sum[n] += x[n][i]; }
+            for (int i = 0; i < 8; ++i) x[n][i] = y[i];
+            load8<T>(src + n * kKv4Group + 8, p.vec, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[n][8 + i] = y[i];
           }
+        } else {
 #pragma unroll
-          for (int o = 1; o < 4; o <<= 1) {
-            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+          for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
-          }
-          // power of two that brings the row's largest element to [2^14, 2^15); a row with an infinity or a NaN makes its scores NaN
-          int e = (int)(__float_as_uint(top) >> 23) - 127;
-          const bool odd = e == 128;
-          e = min(max(e, -112), 126);
-          const float f = pow2(14 - e);
+            for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+        }
+        float top = 0.f, sum[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          sum[n] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) { top = max_nan(top, fabsf(x[n][i])); sum[n] += x[n][i]; }
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+          for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
+        }
+        // power of two that brings the row's largest element to [2^14, 2^15); a row with an infinity or a NaN makes its scores NaN
+        int e = (int)(__float_as_uint(top) >> 23) - 127;
+        const bool odd = e == 128;
+        e = min(max(e, -112), 126);
+        const float f = pow2(14 - e);
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float *y = &x[n][8 * w + 2 * h];   // features 2h, 2h + 4 meet low codes, 2h + 1, 2h + 5 high ones
+              float v[4] = {y[0] * f, y[4] * f, y[1] * f * kHighQ, y[5] * f * kHighQ};
+#pragma unroll
+              for (int sp = 0; sp < NSP; ++sp) {
+                uint32_t (&dst)[2] = qf[nt][sp][n * KS + 2 * w + h];
+                float x4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  x4[i] = sp + 1 < NSP ? grid16(v[i]) : v[i];
+                  v[i] -= x4[i];
+                }
+                dst[0] = half2_bits(x4[0], x4[1]);
+                dst[1] = half2_bits(x4[2], x4[3]);
+              }
+            }
+        // scores: fac * (s_0 acc_0 + s_1 acc_1) + ...
+        const float fac = odd ? __uint_as_float(0x7fc00000u) : p.qk_scale * kLow * pow2(e - 14);
+#pragma unroll
+        for (int col = 0; col < 2; ++col) {
+          qfac[nt][col] = __shfl_sync(0xffffffffu, fac, 4 * (2 * t + col));
+#pragma unroll
+          for (int n = 0; n < NG; ++n) qsum[nt][col][n] = __shfl_sync(0xffffffffu, sum[n] * p.qk_scale, 4 * (2 * t + col));
+        }
+      }
+    }
+    const int vis0 = seq4_visible(u.ahead, u.cap, u.flags & UNIT4_ONE ? 0 : u.r0 / p.G);
+    int vis[NT][2];                        // keys each of this lane's columns may see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int col = 0; col < 2; ++col)
+        vis[nt][col] = u.flags & UNIT4_SAME ? vis0 : seq4_visible(u.ahead, u.cap, (u.r0 + min(nt * 8 + (2 * t + col) % RW, u.nrows - 1)) / p.G);
+
+    float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
+    float lim[NG], pf[NG];                 // E = exponent of the largest value scale so far: 2^(E + 1), 2^(14 - E)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int col = 0; col < 2; ++col) {
+        m[nt][col] = -INFINITY; den[nt][col] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) low[nt][col][n] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < NG; ++n) { lim[n] = pow2(-99); pf[n] = pow2(114); }
+
+    for (int key0 = u.k0; key0 < u.kend; key0 += S::kKeys) {
+      if (issued <= done) copy_next();                                   // (it had to wait for a place among the units)
+      if (S::kRingLen > 2 && issued - done > 1) cp_async_wait<1>();      // this stage has landed; the one after it may be under way
+      else cp_async_wait<0>();
+      __syncwarp();    // ... for every lane, and every lane has read the stage before it
+      ++done;
+      while (issued < done + S::kRingLen - 1 && copy_next()) {}          // whose place is filled again
+      const unsigned char *stage = ring + slot_r * S::kStage;
+      slot_r = slot_r + 1 == S::kRingLen ? 0 : slot_r + 1;
+      const unsigned char *mine = stage + S::block_at(sub);   // this lane's block of set 0 (of set k: block_at(k SUB) further)
+      const int my_key = key0 + 16 * sub + ka;
+      // EDGE: some row does not see all of the stage.  A key that a row does not see may hold a NaN (a later token, or whatever
+      // the page held before): it is kept out of the sums by selection, not by a weight of zero.
+      auto stage_body = [&](auto edge_c) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        // products of the queries with the codes of KB x 16 keys, each lane those of its columns
+        float d[NSET][NT][NG][4];
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+          const unsigned char *blk = stage + S::block_at(j);
+          uint32_t wa[2 * NG], wb[2 * NG];
+          lds_words(blk + F::KC + ka * F::kCodes + t * 8 * NG, wa);
+          lds_words(blk + F::KC + (ka + 8) * F::kCodes + t * 8 * NG, wb);
+          float x[NT][NSP][NG][4];
 #pragma unroll
           for (int n = 0; n < NG; ++n)
 #pragma unroll
             for (int w = 0; w < 2; ++w)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const float *y = &x[n][8 * w + 2 * h];   // features 2h, 2h + 4 meet low codes, 2h + 1, 2h + 5 high ones
-                float v[4] = {y[0] * f, y[4] * f, y[1] * f * kHighQ, y[5] * f * kHighQ};
+                const uint32_t y = wa[2 * n + w] >> (8 * h), z = wb[2 * n + w] >> (8 * h);
+                const uint32_t a0 = code_pair<CEN, 0>(y), a1 = code_pair<CEN, 0>(z), a2 = code_pair<CEN, 1>(y), a3 = code_pair<CEN, 1>(z);
 #pragma unroll
-                for (int sp = 0; sp < NSP; ++sp) {
-                  uint32_t (&dst)[2] = qf[nt][sp][n * KS + 2 * w + h];
-                  float x4[4];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    x4[i] = sp + 1 < NSP ? grid16(v[i]) : v[i];
-                    v[i] -= x4[i];
+                  for (int sp = 0; sp < NSP; ++sp) {
+                    const uint32_t (&q2)[2] = qf[nt][sp][n * KS + 2 * w + h];
+                    if (w == 0 && h == 0) mma_f16_first(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
+                    else mma_f16(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
                   }
-                  dst[0] = half2_bits(x4[0], x4[1]);
-                  dst[1] = half2_bits(x4[2], x4[3]);
-                }
               }
-          // scores: fac * (s_0 acc_0 + s_1 acc_1) + ...
-          const float fac = odd ? __uint_as_float(0x7fc00000u) : p.qk_scale * kLow * pow2(e - 14);
-#pragma unroll
-          for (int col = 0; col < 2; ++col) {
-            qfac[nt][col] = __shfl_sync(0xffffffffu, fac, 4 * (2 * t + col));
-#pragma unroll
-            for (int n = 0; n < NG; ++n) qsum[nt][col][n] = __shfl_sync(0xffffffffu, sum[n] * p.qk_scale, 4 * (2 * t + col));
-          }
-        }
-      }
-      int vis[NT][2];                        // keys each of this lane's columns may see
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int col = 0; col < 2; ++col)
-          vis[nt][col] = u.vis0 == u.vis1 ? u.vis0 : seq4_visible(u.ahead, u.cap, (u.r0 + min(nt * 8 + (2 * t + col) % RW, u.nrows - 1)) / p.G);
-
-      float m[NT][2], den[NT][2], low[NT][2][NG], acc[NT][NG * 4][4];
-      float lim[NG], pf[NG];                 // E = exponent of the largest value scale so far: 2^(E + 1), 2^(14 - E)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int col = 0; col < 2; ++col) {
-          m[nt][col] = -INFINITY; den[nt][col] = 0.f;
-#pragma unroll
-          for (int n = 0; n < NG; ++n) low[nt][col][n] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < NG * 4; ++i) acc[nt][i][0] = acc[nt][i][1] = acc[nt][i][2] = acc[nt][i][3] = 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NG; ++n) { lim[n] = pow2(-99); pf[n] = pow2(114); }
-
-      const int ns = (max(u.kend - u.k0, 0) + S::kKeys - 1) / S::kKeys;
-      for (int si = warp; si < ns; si += kAttn4Warps) {
-        const int key0 = u.k0 + si * S::kKeys;
-        cp_async_wait<S::kRingLen - 2>();
-        __syncwarp();    // the stage is there for every lane, and every lane has read the stage before it
-        copy_next();     // ... whose place is filled again
-        const unsigned char *stage = ring + slot_r * S::kStage;
-        slot_r = slot_r + 1 == S::kRingLen ? 0 : slot_r + 1;
-        const unsigned char *mine = stage + S::block_at(sub);   // this lane's block of set 0 (of set k: block_at(k SUB) further)
-        const int my_key = key0 + 16 * sub + ka;
-        // EDGE: some row does not see all of the stage.  A key that a row does not see may hold a NaN (a later token, or whatever
-        // the page held before): it is kept out of the sums by selection, not by a weight of zero.
-        auto stage_body = [&](auto edge_c) {
-          constexpr bool EDGE = decltype(edge_c)::value;
-          // products of the queries with the codes of KB x 16 keys, each lane those of its columns
-          float d[NSET][NT][NG][4];
-#pragma unroll
-          for (int j = 0; j < KB; ++j) {
-            const unsigned char *blk = stage + S::block_at(j);
-            uint32_t wa[2 * NG], wb[2 * NG];
-            lds_words(blk + F::KC + ka * F::kCodes + t * 8 * NG, wa);
-            lds_words(blk + F::KC + (ka + 8) * F::kCodes + t * 8 * NG, wb);
-            float x[NT][NSP][NG][4];
-#pragma unroll
-            for (int n = 0; n < NG; ++n)
-#pragma unroll
-              for (int w = 0; w < 2; ++w)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const uint32_t y = wa[2 * n + w] >> (8 * h), z = wb[2 * n + w] >> (8 * h);
-                  const uint32_t a0 = code_pair<CEN, 0>(y), a1 = code_pair<CEN, 0>(z), a2 = code_pair<CEN, 1>(y), a3 = code_pair<CEN, 1>(z);
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int sp = 0; sp < NSP; ++sp) {
-                      const uint32_t (&q2)[2] = qf[nt][sp][n * KS + 2 * w + h];
-                      if (w == 0 && h == 0) mma_f16_first(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
-                      else mma_f16(x[nt][sp][n], a0, a1, a2, a3, q2[0], q2[1]);
-                    }
-                }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int n = 0; n < NG; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float y = NSP == 1 ? x[nt][0][n][i] : x[nt][0][n][i] + x[nt][NSP - 1][n][i];
-                  float &to = d[j / SUB][nt][n][i];
-                  to = j % SUB == 0 ? y : sub == j % SUB ? y : to;
-                }
-          }
-          // scores
-          float sc[NSET][NT][4];
-#pragma unroll
-          for (int k = 0; k < NSET; ++k)
-#pragma unroll
-            for (int row = 0; row < 2; ++row) {
-              uint32_t par[NG];
-              lds_words(mine + S::block_at(k * SUB) + F::KP + (ka + 8 * row) * F::kPar, par);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int col = 0; col < 2; ++col) {
-                  float dot = 0.f, off = 0.f;
-#pragma unroll
-                  for (int n = 0; n < NG; ++n) {
-                    dot = fmaf(code_scale(par[n]), d[k][nt][n][2 * row + col], dot);
-                    off = fmaf(code_offset<CEN>(par[n]), qsum[nt][col][n], off);
-                  }
-                  float s = fmaf(qfac[nt][col], dot, off);
-                  if (EDGE && my_key + 16 * SUB * k + 8 * row >= vis[nt][col]) s = -INFINITY;
-                  sc[k][nt][2 * row + col] = s;
-                }
-            }
-
-          // value parameters of this lane's keys; keys that no row of the tile sees count as zeros
-          uint32_t vp[NSET][2][NG];
-          float top[NG], grow[NG];
-#pragma unroll
-          for (int n = 0; n < NG; ++n) { top[n] = 0.f; grow[n] = 1.f; }
-#pragma unroll
-          for (int k = 0; k < NSET; ++k)
-#pragma unroll
-            for (int row = 0; row < 2; ++row) {
-              lds_words(mine + S::block_at(k * SUB) + F::VP + (ka + 8 * row) * F::kPar, vp[k][row]);
-#pragma unroll
-              for (int n = 0; n < NG; ++n) {
-                if (EDGE && my_key + 16 * SUB * k + 8 * row >= u.kend) vp[k][row][n] = 0u;
-                top[n] = fmaxf(top[n], code_scale(vp[k][row][n]));   // (passes over a NaN)
-              }
-            }
-          // a scale of 2^(E + 1) or more raises E
-          bool rescale = false;
-#pragma unroll
-          for (int n = 0; n < NG; ++n) rescale = rescale || top[n] >= lim[n];
-          rescale = __any_sync(0xffffffffu, rescale);
-          if (rescale) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) {
-              const int was = (int)(__float_as_uint(lim[n]) >> 23) - 128;
-              const int e = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top[n])) >> 23) - 127, was), 126);
-              grow[n] = pow2(max(was - e, -126));
-              lim[n] = pow2(e + 1);
-              pf[n] = pow2(14 - e);
-            }
-          }
-
-          // running maximum, probabilities
-          float alpha[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int col = 0; col < 2; ++col) {
-              float x = fmaxf(sc[0][nt][col], sc[0][nt][2 + col]);
+            for (int n = 0; n < NG; ++n)
 #pragma unroll
-              for (int k = 1; k < NSET; ++k) x = fmaxf(x, fmaxf(sc[k][nt][col], sc[k][nt][2 + col]));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-              x = fmaxf(x, m[nt][col]);
-              const float ref = x == -INFINITY ? 0.f : x;   // nothing visible yet: every probability below is exp2(-inf) = 0
-              alpha[nt][col] = ex2(m[nt][col] - ref);
-              rescale = rescale || x != m[nt][col];
-              m[nt][col] = x;
-              float sum = 0.f, lo[NG];
+              for (int i = 0; i < 4; ++i) {
+                const float y = NSP == 1 ? x[nt][0][n][i] : x[nt][0][n][i] + x[nt][NSP - 1][n][i];
+                float &to = d[j / SUB][nt][n][i];
+                to = j % SUB == 0 ? y : sub == j % SUB ? y : to;
+              }
+        }
+        // scores
+        float sc[NSET][NT][4];
 #pragma unroll
-              for (int n = 0; n < NG; ++n) lo[n] = 0.f;
+        for (int k = 0; k < NSET; ++k)
 #pragma unroll
-              for (int k = 0; k < NSET; ++k)
-#pragma unroll
-                for (int row = 0; row < 2; ++row) {
-                  const float pr = ex2(sc[k][nt][2 * row + col] - ref);
-                  sc[k][nt][2 * row + col] = pr;
-                  sum += pr;
-#pragma unroll
-                  for (int n = 0; n < NG; ++n) {
-                    const float off = code_offset<CEN>(vp[k][row][n]);
-                    if (!EDGE || my_key + 16 * SUB * k + 8 * row < vis[nt][col]) lo[n] = fmaf(pr, off, lo[n]);
-                  }
-                }
-              den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
-#pragma unroll
-              for (int n = 0; n < NG; ++n) low[nt][col][n] = fmaf(low[nt][col][n], alpha[nt][col], lo[n]);
-            }
-          if (__any_sync(0xffffffffu, rescale)) {
+          for (int row = 0; row < 2; ++row) {
+            uint32_t par[NG];
+            lds_words(mine + S::block_at(k * SUB) + F::KP + (ka + 8 * row) * F::kPar, par);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int n = 0; n < NG; ++n) {
-                const float f0 = alpha[nt][0] * grow[n], f1 = alpha[nt][1] * grow[n];
+              for (int col = 0; col < 2; ++col) {
+                float dot = 0.f, off = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  acc[nt][n * 4 + i][0] *= f0; acc[nt][n * 4 + i][1] *= f1; acc[nt][n * 4 + i][2] *= f0; acc[nt][n * 4 + i][3] *= f1;
+                for (int n = 0; n < NG; ++n) {
+                  dot = fmaf(code_scale(par[n]), d[k][nt][n][2 * row + col], dot);
+                  off = fmaf(code_offset<CEN>(par[n]), qsum[nt][col][n], off);
                 }
+                float s = fmaf(qfac[nt][col], dot, off);
+                if (EDGE && my_key + 16 * SUB * k + 8 * row >= vis[nt][col]) s = -INFINITY;
+                sc[k][nt][2 * row + col] = s;
               }
           }
 
-          // p s as the 8-column operand of the second product: rows 2t, 2t + 1 (+ 8) of column g
-          uint32_t b[NSET][NG][NT][NSP][2];
+        // value parameters of this lane's keys; keys that no row of the tile sees count as zeros
+        uint32_t vp[NSET][2][NG];
+        float top[NG], grow[NG];
 #pragma unroll
-          for (int k = 0; k < NSET; ++k)
+        for (int n = 0; n < NG; ++n) { top[n] = 0.f; grow[n] = 1.f; }
 #pragma unroll
-            for (int row = 0; row < 2; ++row)
+        for (int k = 0; k < NSET; ++k)
 #pragma unroll
-              for (int n = 0; n < NG; ++n) {
-                const float s = code_scale(vp[k][row][n]) * pf[n];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                  float x0 = sc[k][nt][2 * row] * s, x1 = sc[k][nt][2 * row + 1] * s;
-                  if (EDGE) {
-                    const int key = my_key + 16 * SUB * k + 8 * row;
-                    x0 = key >= vis[nt][0] ? 0.f : x0;
-                    x1 = key >= vis[nt][1] ? 0.f : x1;
-                  }
-                  if (NSP == 2) {
-                    const float h0 = grid16(x0), h1 = grid16(x1);
-                    b[k][n][nt][0][row] = transpose8(half2_bits(h0, h1));
-                    b[k][n][nt][NSP - 1][row] = transpose8(half2_bits(x0 - h0, x1 - h1));
-                  } else {
-                    b[k][n][nt][0][row] = transpose8(half2_bits(x0, x1));
-                  }
-                }
-              }
-          // o += (p s) c
-#pragma unroll
-          for (int j = 0; j < KB; ++j) {
-            const unsigned char *blk = stage + S::block_at(j) + F::VC + g * 4 * NG;
-            uint32_t v[4][NG];               // words of features 8g .. 8g + 7 of the groups, of keys t, t + 4, t + 8, t + 12
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lds_words(blk + (t + 4 * i) * F::kCodes, v[i]);
-            const bool on = SUB == 1 || g / RW == j % SUB;   // column g holds this block's keys
+          for (int row = 0; row < 2; ++row) {
+            lds_words(mine + S::block_at(k * SUB) + F::VP + (ka + 8 * row) * F::kPar, vp[k][row]);
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
-              uint32_t bj[NT][NSP][2];
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int sp = 0; sp < NSP; ++sp)
-#pragma unroll
-                  for (int i = 0; i < 2; ++i) bj[nt][sp][i] = on ? b[j / SUB][n][nt][sp][i] : 0u;
-#pragma unroll
-              for (int hi = 0; hi < 2; ++hi) {
-                const uint32_t x = __byte_perm(v[0][n], v[1][n], hi ? 0x7632 : 0x5410), y = __byte_perm(v[2][n], v[3][n], hi ? 0x7632 : 0x5410);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  // a byte (16 times the high code + the low one) stands for the high code: one mask less, and the low code's sum,
-                  // which is in the same thread, is taken off at the end
-                  const uint32_t xb = CEN ? x >> (8 * h) : h ? __byte_perm(x, 0, 0x4341) : x & 0x00ff00ffu;
-                  const uint32_t yb = CEN ? y >> (8 * h) : h ? __byte_perm(y, 0, 0x4341) : y & 0x00ff00ffu;
-                  const uint32_t a0 = code_pair<CEN, 0>(xb), a1 = CEN ? code_pair<CEN, 1>(xb) : xb;
-                  const uint32_t a2 = code_pair<CEN, 0>(yb), a3 = CEN ? code_pair<CEN, 1>(yb) : yb;
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt) {
-                    float (&o)[4] = acc[nt][n * 4 + 2 * hi + h];
-                    if (NSP == 1) {
-                      mma_f16(o, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
-                    } else {
-                      float e0[4], e1[4];
-                      mma_f16_first(e0, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
-                      mma_f16_first(e1, a0, a1, a2, a3, bj[nt][NSP - 1][0], bj[nt][NSP - 1][1]);
-#pragma unroll
-                      for (int i = 0; i < 4; ++i) o[i] += e0[i] + e1[i];
-                    }
-                  }
-                }
-              }
+              if (EDGE && my_key + 16 * SUB * k + 8 * row >= u.kend) vp[k][row][n] = 0u;
+              top[n] = fmaxf(top[n], code_scale(vp[k][row][n]));   // (passes over a NaN)
             }
           }
-        };
-        if (key0 + S::kKeys > u.vis0) stage_body(std::true_type{});
-        else stage_body(std::false_type{});
-      }
-
-      // ---- join the columns of the four warps ----
-      // a warp leaves its columns in the stage that it has read last (nothing is copied there before its next stage begins)
-      const int out_at = S::kOutInRing ? (warp * S::kRingLen + (slot_r == 0 ? S::kRingLen - 1 : slot_r - 1)) * S::kStage
-                                       : S::kRing + warp * 8 * NT * S::kOutLd * 4;
-      float *om = reinterpret_cast<float *>(attn4_sm + out_at);
-      if (S::kOutInRing) __syncwarp();   // every lane has read it
-      else if (cu != 0) __syncthreads(); // the previous unit's results have been read
-      if (lane == 0) s_tmp[warp] = out_at;
+        // a scale of 2^(E + 1) or more raises E
+        bool rescale = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int n = 0; n < NG; ++n) rescale = rescale || top[n] >= lim[n];
+        rescale = __any_sync(0xffffffffu, rescale);
+        if (rescale) {
 #pragma unroll
-        for (int col = 0; col < 2; ++col) {
-          float l = den[nt][col], lo[NG];
-#pragma unroll
-          for (int n = 0; n < NG; ++n) lo[n] = low[nt][col][n];
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            l += __shfl_xor_sync(0xffffffffu, l, o);
-#pragma unroll
-            for (int n = 0; n < NG; ++n) lo[n] += __shfl_xor_sync(0xffffffffu, lo[n], o);
+          for (int n = 0; n < NG; ++n) {
+            const int was = (int)(__float_as_uint(lim[n]) >> 23) - 128;
+            const int e = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top[n])) >> 23) - 127, was), 126);
+            grow[n] = pow2(max(was - e, -126));
+            lim[n] = pow2(e + 1);
+            pf[n] = pow2(14 - e);
           }
-          if (nt * 8 + (2 * t + col) % RW < u.nrows) {
-            float *dst = om + (nt * 8 + 2 * t + col) * S::kOutLd;
+        }
+
+        // running maximum, probabilities
+        float alpha[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int col = 0; col < 2; ++col) {
+            float x = fmaxf(sc[0][nt][col], sc[0][nt][2 + col]);
+#pragma unroll
+            for (int k = 1; k < NSET; ++k) x = fmaxf(x, fmaxf(sc[k][nt][col], sc[k][nt][2 + col]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            x = fmaxf(x, m[nt][col]);
+            const float ref = x == -INFINITY ? 0.f : x;   // nothing visible yet: every probability below is exp2(-inf) = 0
+            alpha[nt][col] = ex2(m[nt][col] - ref);
+            rescale = rescale || x != m[nt][col];
+            m[nt][col] = x;
+            float sum = 0.f, lo[NG];
+#pragma unroll
+            for (int n = 0; n < NG; ++n) lo[n] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NSET; ++k)
+#pragma unroll
+              for (int row = 0; row < 2; ++row) {
+                const float pr = ex2(sc[k][nt][2 * row + col] - ref);
+                sc[k][nt][2 * row + col] = pr;
+                sum += pr;
+#pragma unroll
+                for (int n = 0; n < NG; ++n) {
+                  const float off = code_offset<CEN>(vp[k][row][n]);
+                  if (!EDGE || my_key + 16 * SUB * k + 8 * row < vis[nt][col]) lo[n] = fmaf(pr, off, lo[n]);
+                }
+              }
+            den[nt][col] = fmaf(den[nt][col], alpha[nt][col], sum);
+#pragma unroll
+            for (int n = 0; n < NG; ++n) low[nt][col][n] = fmaf(low[nt][col][n], alpha[nt][col], lo[n]);
+          }
+        if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
-              // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes, or bytes)
-              const float back = lim[n] * pow2(-15);   // 2^(E - 14)
-              float y[8];
+              const float f0 = alpha[nt][0] * grow[n], f1 = alpha[nt][1] * grow[n];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                y[2 * i] = fmaf(acc[nt][n * 4 + i][col] * kLow, back, lo[n]);
-                const float high = CEN ? acc[nt][n * 4 + i][2 + col] : acc[nt][n * 4 + i][2 + col] - acc[nt][n * 4 + i][col];
-                y[2 * i + 1] = fmaf(high * kHigh, back, lo[n]);
+                acc[nt][n * 4 + i][0] *= f0; acc[nt][n * 4 + i][1] *= f1; acc[nt][n * 4 + i][2] *= f0; acc[nt][n * 4 + i][3] *= f1;
               }
-              reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[0] = make_float4(y[0], y[1], y[2], y[3]);
-              reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[1] = make_float4(y[4], y[5], y[6], y[7]);
             }
-            if (g == 0) { dst[HD] = m[nt][col]; dst[HD + 1] = l; }
+        }
+
+        // p s as the 8-column operand of the second product: rows 2t, 2t + 1 (+ 8) of column g
+        uint32_t b[NSET][NG][NT][NSP][2];
+#pragma unroll
+        for (int k = 0; k < NSET; ++k)
+#pragma unroll
+          for (int row = 0; row < 2; ++row)
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              const float s = code_scale(vp[k][row][n]) * pf[n];
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float x0 = sc[k][nt][2 * row] * s, x1 = sc[k][nt][2 * row + 1] * s;
+                if (EDGE) {
+                  const int key = my_key + 16 * SUB * k + 8 * row;
+                  x0 = key >= vis[nt][0] ? 0.f : x0;
+                  x1 = key >= vis[nt][1] ? 0.f : x1;
+                }
+                if (NSP == 2) {
+                  const float h0 = grid16(x0), h1 = grid16(x1);
+                  b[k][n][nt][0][row] = transpose8(half2_bits(h0, h1));
+                  b[k][n][nt][NSP - 1][row] = transpose8(half2_bits(x0 - h0, x1 - h1));
+                } else {
+                  b[k][n][nt][0][row] = transpose8(half2_bits(x0, x1));
+                }
+              }
+            }
+        // o += (p s) c
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+          const unsigned char *blk = stage + S::block_at(j) + F::VC + g * 4 * NG;
+          uint32_t v[4][NG];               // words of features 8g .. 8g + 7 of the groups, of keys t, t + 4, t + 8, t + 12
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lds_words(blk + (t + 4 * i) * F::kCodes, v[i]);
+          const bool on = SUB == 1 || g / RW == j % SUB;   // column g holds this block's keys
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            uint32_t bj[NT][NSP][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int sp = 0; sp < NSP; ++sp)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) bj[nt][sp][i] = on ? b[j / SUB][n][nt][sp][i] : 0u;
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const uint32_t x = __byte_perm(v[0][n], v[1][n], hi ? 0x7632 : 0x5410), y = __byte_perm(v[2][n], v[3][n], hi ? 0x7632 : 0x5410);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                // a byte (16 times the high code + the low one) stands for the high code: one mask less, and the low code's sum,
+                // which is in the same thread, is taken off at the end
+                const uint32_t xb = CEN ? x >> (8 * h) : h ? __byte_perm(x, 0, 0x4341) : x & 0x00ff00ffu;
+                const uint32_t yb = CEN ? y >> (8 * h) : h ? __byte_perm(y, 0, 0x4341) : y & 0x00ff00ffu;
+                const uint32_t a0 = code_pair<CEN, 0>(xb), a1 = CEN ? code_pair<CEN, 1>(xb) : xb;
+                const uint32_t a2 = code_pair<CEN, 0>(yb), a3 = CEN ? code_pair<CEN, 1>(yb) : yb;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  float (&o)[4] = acc[nt][n * 4 + 2 * hi + h];
+                  if (NSP == 1) {
+                    mma_f16(o, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
+                  } else {
+                    float e0[4], e1[4];
+                    mma_f16_first(e0, a0, a1, a2, a3, bj[nt][0][0], bj[nt][0][1]);
+                    mma_f16_first(e1, a0, a1, a2, a3, bj[nt][NSP - 1][0], bj[nt][NSP - 1][1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] += e0[i] + e1[i];
+                  }
+                }
+              }
+            }
           }
         }
-      __syncthreads();
-      if (u.c < u.nch) {   // (a chunk that no row of the tile sees leaves nothing behind)
-        const int e = tid % HD;
-        for (int r = tid / HD; r < u.nrows; r += kAttn4Threads / HD) {
-          constexpr int NP = kAttn4Warps * SUB;   // parts of a row: warp, then block class
-          auto part = [&](int i) { return reinterpret_cast<const float *>(attn4_sm + s_tmp[i / SUB]) + (NT > 1 ? r : (i % SUB) * RW + r) * S::kOutLd; };
-          float M = -INFINITY;
+      };
+      if (key0 + S::kKeys > vis0) stage_body(std::true_type{});
+      else stage_body(std::false_type{});
+    }
+
+    // ---- join the columns ----
+    // in the stage that has been read last: nothing is copied there before the next stage begins
+    float *om = reinterpret_cast<float *>(ring + (slot_r == 0 ? S::kRingLen - 1 : slot_r - 1) * S::kStage);
+    constexpr int V = HD / 32;             // features of a row that a lane joins
 #pragma unroll
-          for (int i = 0; i < NP; ++i) M = fmaxf(M, part(i)[HD]);
-          const float ref = M == -INFINITY ? 0.f : M;
-          float o = 0.f, l = 0.f;
+    for (int nt = 0; nt < NT; ++nt) {
+      __syncwarp();                        // every lane has read it
 #pragma unroll
-          for (int i = 0; i < NP; ++i) {
-            const float *src = part(i);
-            const float lw = src[HD + 1], f = ex2(src[HD] - ref);
-            if (lw != 0.f) { o = fmaf(f, src[e], o); l = fmaf(f, lw, l); }   // a part that saw nothing is left out; a NaN is not
+      for (int col = 0; col < 2; ++col) {
+        float l = den[nt][col], lo[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) lo[n] = low[nt][col][n];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+          for (int n = 0; n < NG; ++n) lo[n] += __shfl_xor_sync(0xffffffffu, lo[n], o);
+        }
+        if (nt * 8 + (2 * t + col) % RW < u.nrows) {
+          float *dst = om + (2 * t + col) * S::kOutLd;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            // accumulator rows g: features 8g + 2i (low codes), rows g + 8: features 8g + 2i + 1 (high codes, or bytes)
+            const float back = lim[n] * pow2(-15);   // 2^(E - 14)
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              y[2 * i] = fmaf(acc[nt][n * 4 + i][col] * kLow, back, lo[n]);
+              const float high = CEN ? acc[nt][n * 4 + i][2 + col] : acc[nt][n * 4 + i][2 + col] - acc[nt][n * 4 + i][col];
+              y[2 * i + 1] = fmaf(high * kHigh, back, lo[n]);
+            }
+            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[0] = make_float4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<float4 *>(dst + n * kKv4Group + 8 * g)[1] = make_float4(y[4], y[5], y[6], y[7]);
           }
-          const int ri = u.r0 + r, tok = u.tok0 + ri / p.G, hq = u.h * p.G + ri % p.G;
-          const size_t row = (size_t)tok * a.Hq + hq;
-          if (u.nch == 1) {
-            ((T *)a.out)[(size_t)u.l * a.o_ls + row * HD + e] = from_f<T>(l == 0.f ? 0.f : o / l);
-          } else {
-            float *dst = a.part + (((size_t)u.l * a.n_rows * a.Hq + row) * p.nch_max + u.c) * (HD + 4);
-            dst[e] = o;
-            if (e == 0) { dst[HD] = M; dst[HD + 1] = l; }
-          }
+          if (g == 0) { dst[HD] = m[nt][col]; dst[HD + 1] = l; }
         }
       }
-      if (S::kOutInRing) __syncthreads();   // ... and read, before a stage is copied over it
+      __syncwarp();
+      for (int r = nt * 8; r < min(u.nrows, nt * 8 + RW); ++r) {
+        const float *src = om + (r - nt * 8) * S::kOutLd;   // class i of the row's blocks: i RW columns further
+        float M = src[HD];
+#pragma unroll
+        for (int i = 1; i < SUB; ++i) M = fmaxf(M, src[i * RW * S::kOutLd + HD]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float o[V] = {}, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < SUB; ++i) {
+          const float *at = src + i * RW * S::kOutLd;
+          uint32_t w[V];
+          lds_words(reinterpret_cast<const unsigned char *>(at + V * lane), w);
+          const float lw = at[HD + 1], f = ex2(at[HD] - ref);
+          if (lw != 0.f) {   // a class that saw nothing is left out; a NaN is not
+            l = fmaf(f, lw, l);
+#pragma unroll
+            for (int v = 0; v < V; ++v) o[v] = fmaf(f, __uint_as_float(w[v]), o[v]);
+          }
+        }
+        const int ri = u.r0 + r, i1 = u.flags & UNIT4_ONE ? 0 : ri / p.G, tok = u.tok0 + i1, hq = uh * p.G + ri - i1 * p.G;
+        const size_t row = (size_t)tok * a.Hq + hq;
+        if (u.flags & UNIT4_WHOLE) {
+          T *dst = (T *)a.out + (size_t)ul * a.o_ls + row * HD + V * lane;
+#pragma unroll
+          for (int v = 0; v < V; ++v) dst[v] = from_f<T>(l == 0.f ? 0.f : o[v] / l);
+        } else {
+          float *dst = a.part + (((size_t)ul * a.n_rows * a.Hq + row) * p.nch_max + (u.k0 >> p.chunk_sh)) * (HD + 4);
+#pragma unroll
+          for (int v = 0; v < V; ++v) dst[V * lane + v] = o[v];
+          if (lane == 0) { dst[HD] = M; dst[HD + 1] = l; }
+        }
+      }
     }
-    cp_async_wait<0>();
+    finish();
+  }
   }
 }
 
-// Joins the chunks of a row in chunk order: four warps take every fourth chunk each, then the warps in order.
-// grid (rows * Hq, layers), 128 threads.
+// Joins the chunks of a row in chunk order: the warps take every kMergeWarps-th chunk each, then the warps in order.
+// grid (rows * Hq, layers).
+constexpr int kMergeWarps = 8;
 template <typename T, int HD>
-static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant__ Attn4Params p, int tile) {
-  constexpr int V = HD / 32;
-  __shared__ float so[4][HD], sm[4], sl[4];
+static __global__ void __launch_bounds__(32 * kMergeWarps) k_kv4_merge(const __grid_constant__ Attn4Params p, int tile) {
+  constexpr int V = HD / 32, W = kMergeWarps;
+  __shared__ float so[W][HD], sm[W], sl[W];
   const Kv4Attn &a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int tok = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, l = blockIdx.y;
@@ -1266,19 +1303,19 @@ static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant_
   const int i = tok - s.row0;
   if (i < 0 || i >= s.T) return;
   const int ri = i * p.G + hq % p.G, last = min((ri / tile + 1) * tile, s.T * p.G) - 1;
-  if (seq4_visible(s.len - s.T, s.cap, last / p.G) <= p.chunk) return;            // the tile had one chunk: its rows are done
-  const int nch = (seq4_visible(s.len - s.T, s.cap, i) + p.chunk - 1) / p.chunk;
+  if (seq4_visible(s.len - s.T, s.cap, last / p.G) <= 1 << p.chunk_sh) return;            // the tile had one chunk: its rows are done
+  const int nch = (seq4_visible(s.len - s.T, s.cap, i) + (1 << p.chunk_sh) - 1) >> p.chunk_sh;
   const size_t row = (size_t)tok * a.Hq + hq;
   const float *src = a.part + ((size_t)l * a.n_rows * a.Hq + row) * p.nch_max * (HD + 4);
   float o[V] = {}, M = -INFINITY, den = 0.f;
   constexpr int UN = 4;
-  for (int c0 = warp; c0 < nch; c0 += 4 * UN) {
+  for (int c0 = warp; c0 < nch; c0 += W * UN) {
     float x[UN][V], mc[UN], lc[UN];
 #pragma unroll
     for (int k = 0; k < UN; ++k) {
-      const float *at = src + (size_t)(c0 + 4 * k) * (HD + 4);
+      const float *at = src + (size_t)(c0 + W * k) * (HD + 4);
       mc[k] = -INFINITY; lc[k] = 0.f;
-      if (c0 + 4 * k < nch) {
+      if (c0 + W * k < nch) {
         mc[k] = __ldcg(at + HD); lc[k] = __ldcg(at + HD + 1);
 #pragma unroll
         for (int v = 0; v < V; ++v) x[k][v] = __ldcg(at + lane + 32 * v);
@@ -1286,7 +1323,7 @@ static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant_
     }
 #pragma unroll
     for (int k = 0; k < UN; ++k) {
-      if (c0 + 4 * k >= nch || lc[k] == 0.f) continue;
+      if (c0 + W * k >= nch || lc[k] == 0.f) continue;
       const float nm = fmaxf(M, mc[k]), ref = nm == -INFINITY ? 0.f : nm, f = ex2(mc[k] - ref), old = den == 0.f ? 0.f : ex2(M - ref);
 #pragma unroll
       for (int v = 0; v < V; ++v) o[v] = fmaf(f, x[k][v], o[v] * old);
@@ -1299,10 +1336,12 @@ static __global__ void __launch_bounds__(128) k_kv4_merge(const __grid_constant_
   if (lane == 0) { sm[warp] = M; sl[warp] = den; }
   __syncthreads();
   if (threadIdx.x < HD) {
-    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), ref = top == -INFINITY ? 0.f : top;
-    float y = 0.f, d = 0.f;
+    float top = sm[0], y = 0.f, d = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 1; w < W; ++w) top = fmaxf(top, sm[w]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
       if (sl[w] == 0.f) continue;
       const float f = ex2(sm[w] - ref);
       y = fmaf(f, so[w][threadIdx.x], y);

@@ -51,7 +51,6 @@ struct Kv4Attn {
   float scale;
   bool fp32;
 };
-int kv4_chunk(int pairs);                   // keys of a split, from the number of (sequence, key/value head) pairs
 size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl);
 cudaError_t kv4_attention(const Kv4Attn &p, int n_sm, cudaStream_t st);
 int kv4_attention_launches(int B, int Hkv, int max_len);   // kernels of one call

@@ -390,6 +390,15 @@ def test_attention_many_chunks(S, B, n, hk, G):
     run_attention(S, lens, 1, hk * G, hk, 64, 64, F32)
 
 
+def test_attention_long_splits(S):
+    """A length bound beyond 256 splits of 512 keys: splits of 1024, more blocks than lanes."""
+    c = Cache(S, [5000, 1030, 90], 1, 64, 16, F32, width=16385)
+    q, q64 = rounded(np.random.default_rng(2), (3, 2, 64), F32)
+    c.check(c.attend(q), q64, [0, 1, 2, 3], F32)
+    two, q2, q264 = Cache(S, [4100], 2, 128, 64, BF, width=4097), *rounded(np.random.default_rng(3), (20, 2, 128), BF)
+    two.check(two.attend(q2), q264, [0, 20], BF)
+
+
 def test_attention_max_len_cuts_and_scale(S):
     c = Cache(S, [300, 90], 2, 128, 16)
     q, q64 = rounded(np.random.default_rng(2), (2, 2, 128), BF)
