@@ -298,8 +298,9 @@ int snlp_lm_head_greedy_static(const float *hL, const void *lm_head_bf16, int ro
  * Operators of a cache that holds keys and values in 4 bits and requests of different lengths; they need no model
  * handle (snlp_kv_create_4bit is the cache of a model that runs on them).  They use the current CUDA device, which must
  * be the one their pointers belong to, and only enqueue work on `stream`; they allocate nothing, keep nothing between
- * calls and may be captured into CUDA graphs.  The paper has no counterpart: a K-sweep decode step reads the cache K
- * times, which is why a smaller cache pays here.
+ * calls and may be captured into CUDA graphs (the first call on a device sets kernel attributes: make it before a
+ * capture).  The paper has no counterpart: a K-sweep decode step reads the cache K times, which is why a smaller cache
+ * pays here.
  *
  * Format.  The head_dim features (64 or 128) of one token of one head are cut into groups of 64.  A group is 64 codes
  * c in 0..15 and a bf16 pair (s, m): value = s * c + m.  With lo, hi the group's smallest and largest element,
@@ -353,7 +354,7 @@ int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const 
  *         cu_q[B] are left as they are); NULL: n_rows / B rows each
  *   max_len  no length is above it (longer ones are cut); 0 = max_pages * page_size.  It sizes the workspace.
  *   scale  of the scores; 0 = 1/sqrt(head_dim)
- * out [n_rows][n_head][head_dim], q's dtype, dense.  bf16 results: probabilities are rounded to 11 bits before the second
+ * out [n_rows][n_head][head_dim], q's dtype, dense, not overlapping q.  bf16 results: probabilities are rounded to 11 bits before the second
  * product; fp32 results: queries and probabilities are split in two such terms (22 bits); all sums are fp32.
  *   tile_rows  query rows of a sequence and key/value head that are worked on together, 2, 4, 8 or 16; 0 = the smallest that
  *         holds the average.  For one tile_rows a row's result depends on its own query, its visible keys, B * n_kv_head and

@@ -1281,17 +1281,20 @@ static __global__ void __launch_bounds__(kAttn4Threads, (Attn4Cfg<T, HD, RW, NT>
   }
 }
 
-// Joins the chunks of a row in chunk order: the warps take every kMergeWarps-th chunk each, then the warps in order.
-// grid (rows * Hq, layers).
+// Joins the chunks of a row: W warps take every W-th chunk each, in order, then the warps in order.  W is chosen by the largest number
+// of chunks that a call may have and the tile (kv4.cu).
+// grid (rows * Hq * W / kMergeWarps, layers).  Bound by latency: one or two round trips to L2.
 constexpr int kMergeWarps = 8;
-template <typename T, int HD>
+template <typename T, int HD, int W>
 static __global__ void __launch_bounds__(32 * kMergeWarps) k_kv4_merge(const __grid_constant__ Attn4Params p, int tile) {
-  constexpr int V = HD / 32, W = kMergeWarps;
+  constexpr int V = HD / 32, UN = W == 1 ? 8 : 4;
   __shared__ float so[W][HD], sm[W], sl[W];
   const Kv4Attn &a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tok = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, l = blockIdx.y;
+  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, l = blockIdx.y;
+  const long long rid = W == 1 ? (long long)blockIdx.x * kMergeWarps + (threadIdx.x >> 5) : blockIdx.x;
   pdl_wait();
+  if (rid >= (long long)a.n_rows * a.Hq) return;
+  const int tok = (int)(rid / a.Hq), hq = (int)(rid % a.Hq);
   int b;
   if (a.cu) {
     if (tok < a.cu[0] || tok >= a.cu[a.B]) return;   // behind the last sequence
@@ -1308,7 +1311,6 @@ static __global__ void __launch_bounds__(32 * kMergeWarps) k_kv4_merge(const __g
   const size_t row = (size_t)tok * a.Hq + hq;
   const float *src = a.part + ((size_t)l * a.n_rows * a.Hq + row) * p.nch_max * (HD + 4);
   float o[V] = {}, M = -INFINITY, den = 0.f;
-  constexpr int UN = 4;
   for (int c0 = warp; c0 < nch; c0 += W * UN) {
     float x[UN][V], mc[UN], lc[UN];
 #pragma unroll
@@ -1331,6 +1333,12 @@ static __global__ void __launch_bounds__(32 * kMergeWarps) k_kv4_merge(const __g
       M = nm;
     }
   }
+  T *out = (T *)a.out + (size_t)l * a.o_ls + row * HD;
+  if (W == 1) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[lane + 32 * v] = from_f<T>(den == 0.f ? 0.f : o[v] / den);
+    return;
+  }
 #pragma unroll
   for (int v = 0; v < V; ++v) so[warp][lane + 32 * v] = o[v];
   if (lane == 0) { sm[warp] = M; sl[warp] = den; }
@@ -1347,7 +1355,7 @@ static __global__ void __launch_bounds__(32 * kMergeWarps) k_kv4_merge(const __g
       y = fmaf(f, so[w][threadIdx.x], y);
       d = fmaf(f, sl[w], d);
     }
-    ((T *)a.out)[(size_t)l * a.o_ls + row * HD + threadIdx.x] = from_f<T>(d == 0.f ? 0.f : y / d);
+    out[threadIdx.x] = from_f<T>(d == 0.f ? 0.f : y / d);
   }
 }
 

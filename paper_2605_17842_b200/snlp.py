@@ -412,7 +412,8 @@ def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch
     if free_head is not None and free_head.numel() != 1:
         _refuse("free_head must be one int32")
     pc, pn, pt = _dense_ptr("ctx_lens", ctx_lens, i32, dev), _dense_ptr("new_lens", new_lens, i32, dev), _dense_ptr("block_table", block_table, i32, dev)
-    pf, nf = (_dense_ptr("free_pages", free_pages, i32, dev), free_pages.numel()) if free_pages is not None else (None, 0)
+    # (an empty list has no address, but is not the absence of a list: any other address stands in for it)
+    pf, nf = (_dense_ptr("free_pages", free_pages, i32, dev) or pc, free_pages.numel()) if free_pages is not None else (None, 0)
     ph = _dense_ptr("free_head", free_head, i32, dev) if free_head is not None else None
     slots = ctx_lens.new_empty(max_tokens, dtype=torch.int64)
     positions, cu, lens, info = ctx_lens.new_empty(max_tokens), ctx_lens.new_empty(B + 1), ctx_lens.new_empty(B), ctx_lens.new_empty(2)
@@ -423,6 +424,8 @@ def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch
 
 def _kv4_rows(fn, pool, k, v, slots):
     p, dev, n, dt = _kv4_pool_arg(pool), pool.device, slots.numel(), k.dtype
+    if n > 0x7fffffff:
+        _refuse("more than 2^31 - 1 tokens in one call")
     shape = (n, p.n_kv_head, p.head_dim)
     (kt, kh, ke), (vt, vh, ve) = k.stride() if k.dim() == 3 else (0, 0, 0), v.stride() if v.dim() == 3 else (0, 0, 0)
     if k.shape != shape or v.shape != shape or k.device != dev or v.device != dev or v.dtype is not dt or (n and (ke != 1 or ve != 1)):

@@ -77,6 +77,33 @@ def test_plan_edges(S):
     run_plan(S, [31, 0], [1, 33], 32, 34, 2, free_extra=0)    # exactly enough pages
 
 
+def test_plan_with_an_empty_free_list(S):
+    empty = torch.empty(0, dtype=torch.int32, device="cuda")
+    ctx, table = cuda(np.array([15, 4], np.int32)), cuda(np.array([[3, -1], [2, -1]], np.int32))
+    served = S.page_plan(ctx, cuda(np.array([1, 5], np.int32)), table, 16, 6, free_pages=empty)      # no page is needed
+    assert served.info.tolist() == [0, 0] and served.slots.tolist() == [63, 36, 37, 38, 39, 40]
+    refused = S.page_plan(ctx, cuda(np.array([2, 5], np.int32)), table, 16, 7, free_pages=empty)
+    assert refused.info.tolist() == [0, 1] and (refused.slots == -1).all() and (table[:, 1] == -1).all()
+
+
+def test_bindings_refuse_what_they_cannot_pass_on(S):
+    pool = S.kv4_pool(2, 2, 64, 16)
+    k, sl = torch.zeros((3, 2, 64), dtype=BF, device="cuda"), torch.arange(3, device="cuda")
+    q, t, n = torch.zeros((3, 2, 64), dtype=BF, device="cuda"), torch.zeros((3, 1), dtype=torch.int32, device="cuda"), torch.ones(3, dtype=torch.int32, device="cuda")
+    for f in (lambda: S.kv4_write(pool, k[:2], k, sl), lambda: S.kv4_write(pool, k, k.float(), sl), lambda: S.kv4_write(pool, k.half(), k.half(), sl),
+              lambda: S.kv4_write(pool, k, k, sl.int()), lambda: S.kv4_write(pool, k.transpose(1, 2).contiguous().transpose(1, 2), k, sl),
+              lambda: S.kv4_write(pool.flatten(), k, k, sl), lambda: S.kv4_write(pool, k.cpu(), k, sl), lambda: S.kv4_read(pool, sl, 128),
+              lambda: S.kv4_read(pool, sl, 64, torch.float16), lambda: S.kv4_pool(2, 2, 96, 16), lambda: S.kv4_pool(2, 2, 64, 24),
+              lambda: S.kv4_attention(q[:, :, :32], pool, t, n), lambda: S.kv4_attention(q, pool, t, n[:2]), lambda: S.kv4_attention(q, pool, t.long(), n),
+              lambda: S.kv4_attention(q, pool, t, n, cu_q=n), lambda: S.kv4_attention(q[:, :1].contiguous(), pool, t, n), lambda: S.kv4_attention(q, pool, t, n, out=q[:2]),
+              lambda: S.kv4_attention(q, pool, t, n, max_len=-1), lambda: S.kv4_attention(q, pool, t, n, tile_rows=3), lambda: S.kv4_attention(q[:2], pool, t, n),
+              lambda: S.page_plan(n, n, t[:2], 16, 3), lambda: S.page_plan(n, n.long(), t, 16, 3), lambda: S.page_plan(n, n, t, 16, -1), lambda: S.page_plan(n, n, t, 20, 3),
+              lambda: S.page_plan(n, n, t, 16, 3, free_head=n), lambda: S.page_plan(n[:0], n[:0], t[:0], 16, 3)):
+        with pytest.raises(S.SnlpError):
+            f()
+    assert torch.equal(S.kv4_attention(q[:0], pool, t, n, cu_q=torch.zeros(4, dtype=torch.int32, device="cuda")), q[:0])
+
+
 def test_plan_full_table_takes_nothing(S):
     table = np.arange(12, dtype=np.int32).reshape(3, 4)
     table[1, 2] = -1                                    # a hole: its tokens have no slot
@@ -388,6 +415,13 @@ def test_attention_many_chunks(S, B, n, hk, G):
     lens = rng.integers(1, n + 1, B).tolist()
     lens[0] = n
     run_attention(S, lens, 1, hk * G, hk, 64, 64, F32)
+
+
+def test_attention_of_thousands_of_sequences(S):
+    """More sequences than the kernel's list has entries for, empty ones among them."""
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 40, 2500).tolist()
+    run_attention(S, lens, rng.integers(0, 3, 2500).tolist(), 2, 1, 64, 16, F32, ragged=True)
 
 
 def test_attention_long_splits(S):
