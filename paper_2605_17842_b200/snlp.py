@@ -333,6 +333,7 @@ def lm_head_greedy_static(hL: torch.Tensor, lm_head_bf16: torch.Tensor, n_stream
 
 # -- key/value cache held in 4 bits ------------------------------------------------------------------
 KV4_BLOCK = 16                                   # tokens of a storage block
+KV4_MIN_SPLIT = 128                              # keys of the shortest split of the attention
 _KV4_BLOCK_BYTES = {64: 1152, 128: 2304}         # by head_dim: 16 tokens' codes and parameters, keys and values
 _KV4_HEAD_DIM = {v: k for k, v in _KV4_BLOCK_BYTES.items()}
 
@@ -464,7 +465,7 @@ def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor
     if len(tab) != 2 or tab[0] != B or (cu_q is not None and cu_q.numel() != B + 1):
         _refuse("block_table must be [B, max_pages], lens [B], cu_q [B + 1]")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty_like(q) if q.is_contiguous() else torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape:
         _refuse("out must have q's shape")
     qt, qh, _ = q.stride()
@@ -474,11 +475,18 @@ def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor
     po = _dense_ptr("out", out, q.dtype, dev)
     pp, pa, pw, size = C.byref(p), C.byref(a), None, 0
     if workspace is None:
-        need = C.c_size_t()
-        _check(_lib.snlp_kv4_attention_workspace(pp, pa, C.byref(need)))
-        if need.value:
-            workspace = pool.new_empty(need.value)
-    if workspace is not None:
+        # no split is shorter than KV4_MIN_SPLIT keys: where that bound is small, it does without the question
+        keys = tab[1] * p.page_size
+        splits = -(-(min(max_len, keys) if max_len > 0 else keys) // KV4_MIN_SPLIT)
+        size = shape[0] * shape[1] * splits * (p.head_dim + 4) * 4 if splits > 1 else 0
+        if size > 1 << 22:
+            need = C.c_size_t()
+            _check(_lib.snlp_kv4_attention_workspace(pp, pa, C.byref(need)))
+            size = need.value
+        if size:
+            workspace = pool.new_empty(size)
+            pw = workspace.data_ptr()
+    else:
         pw, size = _dense_ptr("workspace", workspace, torch.uint8, dev), workspace.numel()
     _call_on(dev.index, _lib.snlp_kv4_attention, pp, pa, po, pw, size)
     return out
