@@ -29,6 +29,19 @@ static int rows_vec(const Kv4Rows &p) {
   return 0;
 }
 
+// A launch that may carry the programmatic-serialisation attribute: the kernel is set up while the one before it finishes, and waits
+// for that one's results at its own pdl_wait().
+template <typename... KArgs, typename... Args>
+static void launch(bool pdl, void (*kern)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, Args &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
+  cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);   // a failure is picked up by the cudaGetLastError() that follows
+}
+
 static int log2_of(int page) { return 31 - __builtin_clz((unsigned)page); }
 
 template <bool WRITE>
@@ -46,7 +59,7 @@ static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
   const int sh = log2_of(p.page);
 #define KV4_ROWS(T, HD)                                                                 \
   do {                                                                                  \
-    if (WRITE) k_kv4_write<T, HD><<<grid, kWriteThreads(HD), 0, st>>>(p, vec, hpb, sh); \
+    if (WRITE) launch(p.pdl, k_kv4_write<T, HD>, grid, kWriteThreads(HD), 0, st, p, vec, hpb, sh); \
     else k_kv4_read<T, HD><<<grid, kReadThreads, 0, st>>>(p, vec, hpb, sh);             \
   } while (0)
   if (p.fp32) {
@@ -119,21 +132,15 @@ static cudaError_t attn_launch(const Attn4Params &p, int n_sm, cudaStream_t st) 
   // at most this many units; the kernel counts the real ones from the lengths on the device
   const int64_t most = ((int64_t)a.n_rows * p.G / (RW * NT) + a.B) * p.nch_max * a.Hkv * a.nl;
   const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)n_sm * resident));
-  k_kv4_attn<T, HD, RW, NT><<<grid, kAttn4Threads, smem, st>>>(p);
-  if (p.nch_max > 1) {
-    cudaLaunchConfig_t cfg = {};
+  launch(a.pdl, k_kv4_attn<T, HD, RW, NT>, dim3(grid), kAttn4Threads, smem, st, p);
+  if (p.nch_max > 1) {   // scheduled while the splits finish, waits for their results
     // One warp a row where it has its chunks in one go or there are many rows anyway, eight where a single row would wait for them
     // (prompt chunks, 6 x 200 rows x 24 splits: 45.9 us against 52.6; one row x 16 splits x 10 heads: 11.9 against 10.4).  Only what
     // a call shares with the others on its cache decides: tile, pairs, longest length.
     const bool few = p.nch_max <= 8 || (RW * NT >= 8 && a.B * a.Hkv >= 32);
     const int64_t rows = (int64_t)a.n_rows * a.Hq;
-    cfg.gridDim = dim3((unsigned)(few ? (rows + kMergeWarps - 1) / kMergeWarps : rows), a.nl); cfg.blockDim = dim3(32 * kMergeWarps); cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // scheduled while the splits finish, waits for their results
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    if (few) cudaLaunchKernelEx(&cfg, k_kv4_merge<T, HD, 1>, p, RW * NT);
-    else cudaLaunchKernelEx(&cfg, k_kv4_merge<T, HD, kMergeWarps>, p, RW * NT);
+    const dim3 mgrid((unsigned)(few ? (rows + kMergeWarps - 1) / kMergeWarps : rows), a.nl);
+    launch(true, few ? k_kv4_merge<T, HD, 1> : k_kv4_merge<T, HD, kMergeWarps>, mgrid, 32 * kMergeWarps, 0, st, p, RW * NT);
   }
   return cudaGetLastError();
 }

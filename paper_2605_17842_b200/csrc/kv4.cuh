@@ -445,6 +445,8 @@ template <typename T, int HD>
 static __global__ void __launch_bounds__(kWriteThreads(HD)) k_kv4_write(Kv4Rows p, int vec, int hpb, int page_sh) {
   typedef Kv4Fmt<HD> F;
   constexpr int LPR = HD / 16;
+  pdl_wait();
+  pdl_trigger();
   const int j = threadIdx.x % LPR, hg = (p.H + hpb - 1) / hpb, l = blockIdx.y;
   const int h0 = (int)(blockIdx.x % hg) * hpb, h1 = min(h0 + hpb, p.H);
   const long long tok = (long long)(blockIdx.x / hg) * kKv4Block + threadIdx.x / LPR;

@@ -34,6 +34,7 @@ struct Kv4Rows {                            // write: src -> pool; read: pool ->
   int n, H, hd, page, nl;
   int64_t n_slots;                             // pages * page size
   bool fp32;
+  bool pdl;                                    // write: programmatic dependent launch behind the kernel before it
 };
 cudaError_t kv4_write(const Kv4Rows &p, cudaStream_t st);
 cudaError_t kv4_read(const Kv4Rows &p, cudaStream_t st);
@@ -50,6 +51,7 @@ struct Kv4Attn {
   int tile;                                 // query rows of a work unit: 2, 4, 8 or 16; 0 = chosen by the rows of a sequence and kv head
   float scale;
   bool fp32;
+  bool pdl;                                 // programmatic dependent launch behind the kernel before it
 };
 size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl);
 cudaError_t kv4_attention(const Kv4Attn &p, int n_sm, cudaStream_t st);

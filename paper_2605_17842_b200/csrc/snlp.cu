@@ -655,7 +655,7 @@ static Kv4Rows kv4_rows(snlp_model *m, const Fwd &f, int l0) {
 static int kv4_store(snlp_model *m, const Fwd &f, int l0, int nl) {
   Kv4Rows p = kv4_rows(m, f, l0);
   p.k = (char *)f.kc + (size_t)l0 * f.kv_ls * m->esz; p.v = (char *)f.vc + (size_t)l0 * f.kv_ls * m->esz;
-  p.k_ls = p.v_ls = f.kv_ls; p.slots = f.kv4->slots; p.n = f.M; p.nl = nl;
+  p.k_ls = p.v_ls = f.kv_ls; p.slots = f.kv4->slots; p.n = f.M; p.nl = nl; p.pdl = m->pdl_now;
   TimedLaunch tl_(m, f.st, KC_OTHER);
   return kv4_check(kv4_write(p, f.st));
 }
@@ -680,6 +680,7 @@ static int kv4_attend(snlp_model *m, const Fwd &f, int l0, int nl, const void *q
   a.pool_ls = f.kv4->pool_ls; a.table = f.kv4->table; a.tstride = f.kv4->row_pages; a.lens = f.kv4->lens;
   a.T = f.T; a.n_rows = f.M; a.B = f.B; a.Hq = a.Hkv = c.n_head; a.hd = c.head_dim; a.n_pages = f.kv4->n_pages; a.page = kKv4Page;
   a.max_len = f.kv4->max_ctx; a.scale = 1.f / std::sqrt((float)c.head_dim); a.fp32 = c.dtype == SNLP_DTYPE_FP32;
+  a.pdl = m->pdl_now;
   a.tile = 2;   // one tile for single tokens and blocks of them, so that a verify block reproduces the decode steps bit for bit
   // the decode regime has workspace for all layers at once; more rows go layer by layer
   const bool all = f.M <= kDecodeRows;
