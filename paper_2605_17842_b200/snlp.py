@@ -357,7 +357,8 @@ _lib.snlp_kv4_write.argtypes = [_V, _V, _V, _I, _V, _V, _I, _V]
 _lib.snlp_kv4_read.argtypes = _lib.snlp_kv4_write.argtypes
 _lib.snlp_kv4_attention_workspace.argtypes = [_V, _V, _V]
 _lib.snlp_kv4_attention.argtypes = [_V, _V, _V, _V, _Z, _V]
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_Strides = C.c_int64 * 4
 
 
 def _call_on(index, fn, *args):
@@ -417,10 +418,11 @@ def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch
     pf, nf = (_dense_ptr("free_pages", free_pages, i32, dev) or pc, free_pages.numel()) if free_pages is not None else (None, 0)
     ph = _dense_ptr("free_head", free_head, i32, dev) if free_head is not None else None
     slots = ctx_lens.new_empty(max_tokens, dtype=torch.int64)
-    positions, cu, lens, info = ctx_lens.new_empty(max_tokens), ctx_lens.new_empty(B + 1), ctx_lens.new_empty(B), ctx_lens.new_empty(2)
-    _call_on(dev.index, _lib.snlp_page_plan, pc, pn, B, page_size, pf, nf, ph, pt, shape[1], max_tokens, slots.data_ptr(), positions.data_ptr(),
-             cu.data_ptr(), lens.data_ptr(), info.data_ptr())
-    return PagePlan(slots, positions, cu, lens, info)
+    ints = ctx_lens.new_empty(max_tokens + 2 * B + 3)     # the int32 results, in one piece
+    at = ints.data_ptr()
+    positions, cu, lens, info = at, at + 4 * max_tokens, at + 4 * (max_tokens + B + 1), at + 4 * (max_tokens + 2 * B + 1)
+    _call_on(dev.index, _lib.snlp_page_plan, pc, pn, B, page_size, pf, nf, ph, pt, shape[1], max_tokens, slots.data_ptr(), positions, cu, lens, info)
+    return PagePlan(slots, *ints.split_with_sizes((max_tokens, B + 1, B, 2)))
 
 
 def _kv4_rows(fn, pool, k, v, slots):
@@ -428,10 +430,14 @@ def _kv4_rows(fn, pool, k, v, slots):
     if n > 0x7fffffff:
         _refuse("more than 2^31 - 1 tokens in one call")
     shape = (n, p.n_kv_head, p.head_dim)
-    (kt, kh, ke), (vt, vh, ve) = k.stride() if k.dim() == 3 else (0, 0, 0), v.stride() if v.dim() == 3 else (0, 0, 0)
-    if k.shape != shape or v.shape != shape or k.device != dev or v.device != dev or v.dtype is not dt or (n and (ke != 1 or ve != 1)):
+    strides = None                               # dense
+    ok = k.shape == shape and v.shape == shape and k.device == dev and v.device == dev and v.dtype is dt
+    if ok and not (k.is_contiguous() and v.is_contiguous()):
+        (kt, kh, ke), (vt, vh, ve) = k.stride(), v.stride()
+        ok, strides = ke == 1 and ve == 1, _Strides(kt, kh, vt, vh)
+    if not ok:
         _refuse(f"k and v must be {list(shape)} ([tokens, heads, head_dim], one slot per token) of one dtype on the pool's device, features contiguous")
-    _call_on(dev.index, fn, C.byref(p), k.data_ptr(), v.data_ptr(), _kv4_dtype(dt), (C.c_int64 * 4)(kt, kh, vt, vh),
+    _call_on(dev.index, fn, C.byref(p), k.data_ptr(), v.data_ptr(), _kv4_dtype(dt), strides,
              _dense_ptr("slots", slots, torch.int64, dev), n)
 
 
@@ -447,7 +453,7 @@ def kv4_read(pool: torch.Tensor, slots: torch.Tensor, head_dim: int, dtype=torch
     if k is None or v is None:
         shape = (slots.numel(), pool.shape[1], head_dim)
         k = pool.new_empty(shape, dtype=dtype) if k is None else k
-        v = torch.empty_like(k, memory_format=torch.contiguous_format) if v is None else v
+        v = torch.empty_like(k) if v is None and k.is_contiguous() else pool.new_empty(shape, dtype=dtype) if v is None else v
     _kv4_rows(_lib.snlp_kv4_read, pool, k, v, slots)
     return k, v
 
