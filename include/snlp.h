@@ -175,7 +175,7 @@ int snlp_kv_create(snlp_model *m, int B, int max_ctx, snlp_kv **out);
  * 4 bits before any query sees them, so K = L sweeps still equal sequential execution and a verify block the decode steps it
  * checks.  For prompts of bf16 models it keeps one layer's rows in bf16 beside it; a cache made before the weights are loaded
  * does without and takes longer over prompts.
- * Errors: ARG, SHAPE (B > max_batch or 4096, max_ctx > config.max_ctx), UNSUPPORTED (head_dim), OOM, CUDA. */
+ * Errors: ARG, SHAPE (B > max_batch or 4096, max_ctx > config.max_ctx, 2^31 pages of 64 tokens or more), UNSUPPORTED (head_dim), OOM, CUDA. */
 int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **out);
 int snlp_kv_destroy(snlp_kv *kv);
 /* The length is kept on the device and mirrored on the host.  After snlp_draft_and_verify_async the host knows only an
@@ -326,12 +326,12 @@ int snlp_kv4_pool_bytes(const snlp_kv4_pool *pool, size_t *bytes);
  * only read, the others left as they are.  free_pages == NULL: no page is taken, the table already has them all.
  *   slots     [max_tokens] int64: of the new tokens, sequence after sequence; -1 from the last token on
  *   positions [max_tokens] (nullable): their positions; -1 likewise        cu_new [B+1] (nullable): prefix sums of new_lens
- *   lens      [B]: ctx + new (not one of the inputs)                       info [2] (nullable): pages taken, status
+ *   lens      [B]: ctx + new                                               info [2] (nullable): pages taken, status
  * status 0: served.  Otherwise nothing is taken or entered, every slot and position is -1, cu_new is 0 and lens = ctx (0 where
  * negative); bits: 1 too few free pages, 2 a row needs more than max_pages pages, 4 more than max_tokens new tokens,
  * 8 a negative length or a position beyond int32.  All pointers are device memory; free_head (nullable = 0) is read, not
- * advanced: the caller adds info[0].  A negative table entry gives slot -1.
- * Errors: ARG (NULL, misaligned, page_size, sizes), SHAPE (B > 4096, max_tokens > 2^30), CUDA. */
+ * advanced: the caller adds info[0] once the call is done.  A negative table entry gives slot -1.
+ * Errors: ARG (NULL, misaligned, page_size, sizes, an input that overlaps a result), SHAPE (B > 4096, max_tokens > 2^30), CUDA. */
 int snlp_page_plan(const int32_t *ctx_lens, const int32_t *new_lens, int B, int page_size, const int32_t *free_pages, int n_free,
                    const int32_t *free_head, int32_t *block_table, int max_pages, int max_tokens, int64_t *slots,
                    int32_t *positions, int32_t *cu_new, int32_t *lens, int32_t *info, void *stream);
@@ -343,7 +343,8 @@ int snlp_page_plan(const int32_t *ctx_lens, const int32_t *new_lens, int B, int 
  * Errors: ARG (NULL, misaligned, dtype, page_size, negative n or stride), UNSUPPORTED (head_dim), SHAPE, CUDA. */
 int snlp_kv4_write(const snlp_kv4_pool *pool, const void *k, const void *v, int dtype, const int64_t *strides, const int64_t *slots, int n,
                    void *stream);
-/* The rows at slots [n] as k, v (rounded to dtype; strides as in snlp_kv4_write); zeros where a slot lies outside the pool. */
+/* The rows at slots [n] as k, v (rounded to dtype; strides as in snlp_kv4_write, at least head_dim where there are two rows);
+ * zeros where a slot lies outside the pool.  The same errors. */
 int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const int64_t *strides, const int64_t *slots, int n, void *stream);
 
 /* Causal attention over the pages.  Sequence b has lens[b] keys (its new rows' among them: write first, then attend) and
@@ -353,7 +354,7 @@ int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const 
  *   cu_q  device int32 [B+1], nullable: rows cu_q[b] .. cu_q[b+1]-1 of q and out are sequence b's (ascending; rows behind
  *         cu_q[B] are left as they are); NULL: n_rows / B rows each
  *   max_len  no length is above it (longer ones are cut); 0 = max_pages * page_size.  It sizes the workspace.
- *   scale  of the scores; 0 = 1/sqrt(head_dim)
+ *   scale  of the scores, finite; 0 = 1/sqrt(head_dim)
  * out [n_rows][n_head][head_dim], q's dtype, dense, not overlapping q.  bf16 results: probabilities are rounded to 11 bits before the second
  * product; fp32 results: queries and probabilities are split in two such terms (22 bits); all sums are fp32.
  *   tile_rows  query rows of a sequence and key/value head that are worked on together, 2, 4, 8 or 16; 0 = the smallest that

@@ -2,6 +2,7 @@
 #include "../../include/snlp.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <mutex>
@@ -226,7 +227,13 @@ extern "C" int snlp_page_plan(const int32_t *ctx_lens, const int32_t *new_lens, 
   if (B < 1 || max_pages < 1 || max_tokens < 0 || n_free < 0) return refuse(SNLP_ERR_ARG, "%s: B and max_pages must be >= 1, max_tokens and n_free >= 0", who);
   if (B > kKv4MaxBatch) return refuse(SNLP_ERR_SHAPE, "%s: B = %d exceeds %d", who, B, kKv4MaxBatch);
   if (max_tokens > (1 << 30)) return refuse(SNLP_ERR_SHAPE, "%s: max_tokens = %d exceeds %d", who, max_tokens, 1 << 30);
-  if (lens == ctx_lens || lens == new_lens) return refuse(SNLP_ERR_ARG, "%s: lens must not be one of the inputs", who);
+  // every block reads the inputs while others write the results
+  const struct { const void *p; int64_t bytes; } in[4] = {{ctx_lens, 4LL * B}, {new_lens, 4LL * B}, {free_pages, 4LL * n_free}, {free_head, 4}},
+      res[6] = {{block_table, 4LL * B * max_pages}, {slots, 8LL * max_tokens}, {positions, 4LL * max_tokens}, {cu_new, 4LL * (B + 1)}, {lens, 4LL * B}, {info, 8}};
+  for (const auto &x : in)
+    for (const auto &y : res)
+      if (x.p && y.p && (uintptr_t)x.p < (uintptr_t)y.p + y.bytes && (uintptr_t)y.p < (uintptr_t)x.p + x.bytes)
+        return refuse(SNLP_ERR_ARG, "%s: an input (lengths, free_pages, free_head) overlaps a result", who);
   int rc = check_page(page_size, who);
   if (rc != SNLP_OK) return rc;
   if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
@@ -256,6 +263,10 @@ static int rows_call(bool write, const snlp_kv4_pool *pool, void *k, void *v, in
     if (s[i] < 0) return refuse(SNLP_ERR_ARG, "%s: strides must be >= 0", who);
   p.k_ts = s[0]; p.k_hs = s[1]; p.v_ts = s[2]; p.v_hs = s[3];
   p.pool = (uint8_t *)pool->pages; p.slots = slots; p.n = n; p.H = pool->n_kv_head; p.hd = pool->head_dim; p.page = pool->page_size;
+  if (!write) {   // rows that share memory would be written by several blocks at once
+    auto apart = [&](size_t ts, size_t hs) { return (n < 2 || ts >= (size_t)p.hd) && (p.H < 2 || hs >= (size_t)p.hd); };
+    if (k == v || !apart(p.k_ts, p.k_hs) || !apart(p.v_ts, p.v_hs)) return refuse(SNLP_ERR_ARG, "%s: rows of the output overlap", who);
+  }
   p.n_slots = (int64_t)pool->n_pages * pool->page_size;
   p.fp32 = dtype == SNLP_DTYPE_FP32;
   if ((int64_t)((n + (int64_t)kKv4Block - 1) / kKv4Block) * p.H > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
@@ -312,7 +323,7 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   if ((uintptr_t)args->q % es || (uintptr_t)out % es || (uintptr_t)args->block_table % 4 || (uintptr_t)args->lens % 4 || (uintptr_t)args->cu_q % 4)
     return refuse(SNLP_ERR_ARG, "%s: q and out must be aligned to their element, int32 arrays to 4 bytes", who);
   if (args->q_token_stride < 0 || args->q_head_stride < 0) return refuse(SNLP_ERR_ARG, "%s: strides must be >= 0", who);
-  if (!(args->scale == args->scale)) return refuse(SNLP_ERR_ARG, "%s: scale is not a number", who);
+  if (!std::isfinite(args->scale)) return refuse(SNLP_ERR_ARG, "%s: scale is not a finite number", who);
   Kv4Attn a{};
   a.max_len = attn_max_len(args, pool);
   const size_t need = kv4_workspace(args->n_rows, args->B, args->n_head, pool->n_kv_head, pool->head_dim, a.max_len, 1);

@@ -1371,11 +1371,26 @@ extern "C" int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **
   if (B > c.max_batch || B > kKv4MaxBatch) return fail(SNLP_ERR_SHAPE, "snlp_kv_create_4bit: B = %d exceeds %d", B, std::min(c.max_batch, kKv4MaxBatch));
   if (max_ctx > c.max_ctx) return fail(SNLP_ERR_SHAPE, "snlp_kv_create_4bit: max_ctx = %d exceeds the model's %d", max_ctx, c.max_ctx);
   if (c.head_dim != 64 && c.head_dim != 128) return fail(SNLP_ERR_UNSUPPORTED, "snlp_kv_create_4bit: head_dim must be 64 or 128 (got %d)", c.head_dim);
+  const int64_t row_pages = ((int64_t)max_ctx + kKv4Page - 1) / kKv4Page;
+  if (B * row_pages > 0x7fffffffLL) return fail(SNLP_ERR_SHAPE, "snlp_kv_create_4bit: B * max_ctx = %lld positions are too many", (long long)B * max_ctx);
+  // page of every (sequence, page of its row): sequence b has pages b * row_pages ..; slots of every position
+  std::vector<int32_t> table;
+  std::vector<int64_t> slots;
+  try {
+    table.resize(B * row_pages);
+    slots.resize((size_t)B * max_ctx);
+    m->caches.reserve(m->caches.size() + 1);
+  } catch (const std::exception &) {
+    return fail(SNLP_ERR_OOM, "snlp_kv_create_4bit: host allocation failed");
+  }
+  std::iota(table.begin(), table.end(), 0);
+  for (int b = 0; b < B; ++b)
+    for (int p = 0; p < max_ctx; ++p) slots[(size_t)b * max_ctx + p] = b * row_pages * kKv4Page + p;
   snlp_kv *kv = new (std::nothrow) snlp_kv;
   if (!kv) return fail(SNLP_ERR_OOM, "snlp_kv_create_4bit: host allocation failed");
   kv->m = m; kv->B = B; kv->max_ctx = max_ctx;
-  kv->row_pages = (max_ctx + kKv4Page - 1) / kKv4Page;
-  kv->n_pages = B * kv->row_pages;
+  kv->row_pages = (int)row_pages;
+  kv->n_pages = (int)table.size();
   kv->pool_ls = (size_t)kv->n_pages * c.n_head * (kKv4Page / kKv4Block) * kv4_block_bytes(c.head_dim);
   const size_t pool = c.n_layer * kv->pool_ls;
   const bool prompts = m->have_wmaps && c.dtype == SNLP_DTYPE_BF16 && c.head_dim == 128;   // the tensor-core prompt attention serves this model
@@ -1391,18 +1406,13 @@ extern "C" int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **
     kv_free(kv);
     return fail(SNLP_ERR_OOM, "snlp_kv_create_4bit: cudaMalloc of %zu bytes failed", pool + 2 * dense + part);
   }
-  // the table gives sequence b the pages b * row_pages ..; a page that was never written holds zeros, so that nothing read
-  // beyond a length is a NaN
-  std::vector<int32_t> table(kv->n_pages);
-  std::vector<int64_t> slots((size_t)B * max_ctx);
-  std::iota(table.begin(), table.end(), 0);
-  for (int b = 0; b < B; ++b)
-    for (int p = 0; p < max_ctx; ++p) slots[(size_t)b * max_ctx + p] = (int64_t)b * kv->row_pages * kKv4Page + p;
+  // a page that was never written holds zeros, so that nothing read beyond a length is a NaN
   ok = cudaMemset(kv->pool, 0, pool) == cudaSuccess && cudaMemset(kv->pos, 0, 16) == cudaSuccess &&
        cudaMemcpy(kv->table, table.data(), table.size() * 4, cudaMemcpyHostToDevice) == cudaSuccess &&
        cudaMemcpy(kv->all_slots, slots.data(), slots.size() * 8, cudaMemcpyHostToDevice) == cudaSuccess;
   if (ok && dense) ok = cudaMemset(kv->k, 0, dense) == cudaSuccess && cudaMemset(kv->v, 0, dense) == cudaSuccess;
-  if (ok) ok = kv4_init() == cudaSuccess;
+  // the default stream's fills end before any stream of the caller's may write the pages
+  if (ok) ok = kv4_init() == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
     kv_free(kv);

@@ -359,6 +359,7 @@ _lib.snlp_kv4_attention_workspace.argtypes = [_V, _V, _V]
 _lib.snlp_kv4_attention.argtypes = [_V, _V, _V, _V, _Z, _V]
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _Strides = C.c_int64 * 4
+_INT_MAX = 0x7fffffff
 
 
 def _call_on(index, fn, *args):
@@ -409,8 +410,8 @@ def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch
     block_table [B, max_pages] is completed in place with pages from free_pages[free_head:] (None: it has them all).
     max_tokens: length of the slot map, at least the number of new tokens."""
     dev, B, shape, i32 = ctx_lens.device, ctx_lens.numel(), block_table.shape, torch.int32
-    if not ctx_lens.is_cuda or len(shape) != 2 or shape[0] != B or new_lens.numel() != B or max_tokens < 0:
-        _refuse("ctx_lens, new_lens [B] and block_table [B, max_pages] must be cuda tensors of one batch, max_tokens >= 0")
+    if not ctx_lens.is_cuda or len(shape) != 2 or shape[0] != B or new_lens.numel() != B or not 0 <= max_tokens <= _INT_MAX:
+        _refuse("ctx_lens, new_lens [B] and block_table [B, max_pages] must be cuda tensors of one batch, max_tokens >= 0 and an int32")
     if free_head is not None and free_head.numel() != 1:
         _refuse("free_head must be one int32")
     pc, pn, pt = _dense_ptr("ctx_lens", ctx_lens, i32, dev), _dense_ptr("new_lens", new_lens, i32, dev), _dense_ptr("block_table", block_table, i32, dev)
@@ -427,7 +428,7 @@ def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch
 
 def _kv4_rows(fn, pool, k, v, slots):
     p, dev, n, dt = _kv4_pool_arg(pool), pool.device, slots.numel(), k.dtype
-    if n > 0x7fffffff:
+    if n > _INT_MAX:
         _refuse("more than 2^31 - 1 tokens in one call")
     shape = (n, p.n_kv_head, p.head_dim)
     strides = None                               # dense
@@ -470,6 +471,8 @@ def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor
         _refuse("q must be [rows, n_head, head_dim] on the pool's device, features contiguous")
     if len(tab) != 2 or tab[0] != B or (cu_q is not None and cu_q.numel() != B + 1):
         _refuse("block_table must be [B, max_pages], lens [B], cu_q [B + 1]")
+    if not 0 <= max_len <= _INT_MAX or scale == 0:
+        _refuse("max_len must be 0 .. 2^31 - 1, scale not 0")
     if out is None:
         out = torch.empty_like(q) if q.is_contiguous() else torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != shape:

@@ -102,5 +102,5 @@ def attention(q, k, v, length, scale):
                 s = (kk[:vis] @ q[i, h]) * scale
                 w = np.exp(s - s.max())
                 out[i, h] = (w @ vv[:vis]) / w.sum()
-                mag[i, h] = scale * (np.abs(kk[:vis]) @ np.abs(q[i, h])).max()
+                mag[i, h] = abs(scale) * (np.abs(kk[:vis]) @ np.abs(q[i, h])).max()
     return out, mag

@@ -104,6 +104,17 @@ def test_bindings_refuse_what_they_cannot_pass_on(S):
     assert torch.equal(S.kv4_attention(q[:0], pool, t, n, cu_q=torch.zeros(4, dtype=torch.int32, device="cuda")), q[:0])
 
 
+def test_bindings_refuse_what_ctypes_would_cut(S):
+    pool = S.kv4_pool(2, 2, 64, 16)
+    q, t, n = torch.zeros((3, 2, 64), dtype=BF, device="cuda"), torch.zeros((3, 1), dtype=torch.int32, device="cuda"), torch.ones(3, dtype=torch.int32, device="cuda")
+    sl, one = torch.arange(3, device="cuda"), torch.zeros((1, 2, 64), dtype=BF, device="cuda")
+    for f in (lambda: S.kv4_attention(q, pool, t, n, max_len=(1 << 32) + 16), lambda: S.kv4_attention(q, pool, t, n, scale=0.0),
+              lambda: S.kv4_attention(q, pool, t, n, scale=float("inf")), lambda: S.page_plan(n, n, t, 16, (1 << 32) + 3),
+              lambda: S.kv4_read(pool, sl, 64, k=one.expand(3, 2, 64)), lambda: S.kv4_read(pool, sl, 64, k=q, v=q)):
+        with pytest.raises(S.SnlpError):
+            f()
+
+
 def test_plan_full_table_takes_nothing(S):
     table = np.arange(12, dtype=np.int32).reshape(3, 4)
     table[1, 2] = -1                                    # a hole: its tokens have no slot
@@ -440,6 +451,14 @@ def test_attention_max_len_cuts_and_scale(S):
     c.check(c.attend(q, max_len=4000, scale=0.31), q64, [0, 1, 2], BF, scale=0.31)
     wide = Cache(S, [300, 90], 2, 128, 16, width=700)        # a table far wider than the lengths
     wide.check(wide.attend(q), q64, [0, 1, 2], BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [-0.2, 1e-6, -0.03125])
+def test_attention_takes_any_scale(S, scale, dtype):
+    c = Cache(S, [300, 90, 17], 2, 64, 32, dtype)
+    q, q64 = rounded(np.random.default_rng(3), (3, 4, 64), dtype)
+    c.check(c.attend(q, scale=scale), q64, [0, 1, 2, 3], dtype, scale=scale)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

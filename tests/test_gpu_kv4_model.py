@@ -233,3 +233,23 @@ def test_refusals():
     with pytest.raises(snlp.SnlpError):
         kv.truncate(0)
     kv.close()
+
+
+def test_a_new_cache_is_ready_for_any_stream():
+    """A prompt on a stream that does not wait for the default one, right after a large cache was made: its pages and the
+    unpacked rows have been cleared before, not while it runs."""
+    W = synth.make_weights(BF16, seed=3, std=0.05, embed_std=1.0)
+    m = make_model(BF16, W, max_rows=400, max_batch=8, max_ctx=1 << 18)
+    ids = dev(synth.make_ids(BF16, 8, 50, seed=4))
+    want = m.prefill(kv := m.kv_cache(8, 64, bits=4), ids).clone()
+    trace = m.copy_trace(400).clone()
+    kv.close()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        kv = m.kv_cache(8, 1 << 18, bits=4)
+        with torch.cuda.stream(side):
+            got = m.prefill(kv, ids)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(m.copy_trace(400), trace)
+        kv.close()

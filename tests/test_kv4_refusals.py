@@ -91,3 +91,29 @@ def test_attention():
     assert lib.snlp_kv4_attention_workspace(C.byref(pool(pages=None)), C.byref(attn(max_pages=100, max_len=128)), C.byref(n)) == 0 and n.value == 0
     assert lib.snlp_kv4_attention_workspace(C.byref(pool()), C.byref(attn(n_head=3)), C.byref(n)) == snlp.ERR_ARG
     assert go(n_rows=0, q=None, out=0) == 0                  # no row: nothing to do
+
+
+def test_plan_operands_that_overlap():
+    """Blocks read the lengths, the free list and its head while others write the results: they may not share memory."""
+    at = dict(ctx=P, new=P + 64, free=P + 128, head=P + 192, table=2 * P, slots=3 * P, pos=4 * P, cu=5 * P, lens=6 * P, info=7 * P)
+
+    def go(B=4097, **kw):
+        a = {k: C.c_void_p(v) for k, v in {**at, **kw}.items()}
+        return lib.snlp_page_plan(a["ctx"], a["new"], B, 16, a["free"], 4, a["head"], a["table"], 4, 8, a["slots"], a["pos"], a["cu"], a["lens"], a["info"], None)
+    for bad in (dict(lens=P - 4), dict(lens=P + 4), dict(lens=P + 60), dict(info=P + 192), dict(info=P + 188), dict(pos=P + 100), dict(slots=P + 8), dict(cu=P + 136),
+                dict(free=2 * P + 28), dict(head=7 * P + 4), dict(table=P - 28), dict(ctx=4 * P + 28)):
+        assert go(B=2, **bad) == snlp.ERR_ARG and "overlaps" in message(), bad
+
+
+def test_read_into_rows_that_overlap():
+    go = lambda st, v=2 * P, n=2, **kw: lib.snlp_kv4_read(C.byref(pool(**kw)), C.c_void_p(P), C.c_void_p(v), 1, (C.c_int64 * 4)(*st), C.c_void_p(P), n, None)  # noqa: E731
+    for bad in ((0, 64, 128, 64), (128, 0, 128, 64), (128, 64, 63, 64), (128, 64, 128, 32)):
+        assert go(bad) == snlp.ERR_ARG and "overlap" in message(), bad
+    assert go((128, 64, 128, 64), v=P) == snlp.ERR_ARG and "overlap" in message()
+    assert go((0, 63, 0, 64), n=1) == snlp.ERR_ARG                            # one token, two heads
+
+
+@pytest.mark.parametrize("scale", [float("inf"), float("-inf"), float("nan")])
+def test_scale_has_to_be_finite(scale):
+    assert lib.snlp_kv4_attention(C.byref(pool()), C.byref(attn(scale=scale)), C.c_void_p(P), C.c_void_p(P), C.c_size_t(1 << 40), None) == snlp.ERR_ARG
+    assert "scale" in message()
