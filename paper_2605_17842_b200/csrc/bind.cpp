@@ -1,0 +1,307 @@
+// Native half of the Python binding for the per-step operators of the 4-bit cache (snlp_page_plan, snlp_kv4_*): argument checks,
+// results from torch's allocator, one C call on the current stream of the tensors' device.  These calls come once per layer or
+// step and their kernels take 2 .. 10 us, about what the interpreter would need for the checks and allocations alone (page plan
+// plan 16.6 us in Python, 8.1 here).  Signatures and documentation stand in snlp.py.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
+
+#include <cmath>
+#include <limits>
+#include <optional>
+
+#include "../../include/snlp.h"
+
+namespace {
+
+constexpr int64_t kBlock = 16;   // tokens of a storage block
+
+PyObject *g_refuse = nullptr, *g_check = nullptr;   // raise SnlpError: of a message; of a return code
+
+[[noreturn]] void refuse(const char *msg) {
+  Py_XDECREF(PyObject_CallFunction(g_refuse, "s", msg));
+  throw python_error();
+}
+void check(int rc) {
+  if (rc == SNLP_OK) return;
+  Py_XDECREF(PyObject_CallFunction(g_check, "i", rc));
+  throw python_error();
+}
+
+const at::Tensor &tensor(PyObject *o, const char *what) {
+  if (!THPVariable_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s must be a tensor, not %s", what, Py_TYPE(o)->tp_name);
+    throw python_error();
+  }
+  return THPVariable_Unpack(o);
+}
+int64_t integer(PyObject *o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+int int32(PyObject *o, const char *what) {
+  const int64_t v = integer(o);
+  if (v < std::numeric_limits<int>::min() || v > std::numeric_limits<int>::max()) {
+    char msg[128];
+    snprintf(msg, sizeof msg, "%s = %lld is beyond int32", what, (long long)v);
+    refuse(msg);
+  }
+  return (int)v;
+}
+int int32(int64_t v, const char *what) {
+  if (v > std::numeric_limits<int>::max()) {
+    char msg[128];
+    snprintf(msg, sizeof msg, "%s = %lld is beyond int32", what, (long long)v);
+    refuse(msg);
+  }
+  return (int)v;
+}
+
+// address of a dense tensor of one dtype on one device
+void *dense(const char *what, const at::Tensor &t, at::ScalarType dtype, c10::Device dev) {
+  if (t.scalar_type() != dtype || t.device() != dev || !t.is_contiguous()) {
+    char msg[160];
+    snprintf(msg, sizeof msg, "%s must be a contiguous %s tensor on %s", what, c10::toString(dtype), dev.str().c_str());
+    refuse(msg);
+  }
+  return t.data_ptr();
+}
+
+snlp_kv4_pool pool_of(const at::Tensor &t) {
+  const int64_t block = t.dim() == 4 ? t.size(3) : 0;
+  if (t.scalar_type() != at::kByte || !t.is_cuda() || !t.is_contiguous() || (block != 1152 && block != 2304))
+    refuse("pool must be a contiguous cuda uint8 tensor shaped as kv4_pool makes it");
+  snlp_kv4_pool p{};
+  p.pages = t.data_ptr();
+  p.n_pages = int32(t.size(0), "n_pages"); p.n_kv_head = int32(t.size(1), "n_kv_head"); p.page_size = int32(t.size(2) * kBlock, "page_size");
+  p.head_dim = block == 1152 ? 64 : 128;
+  return p;
+}
+
+int dtype_of(at::ScalarType t) {
+  if (t == at::kBFloat16) return SNLP_DTYPE_BF16;
+  if (t == at::kFloat) return SNLP_DTYPE_FP32;
+  refuse("keys, values and queries are bfloat16 or float32");
+}
+
+at::Tensor empty(c10::IntArrayRef shape, at::ScalarType dtype, c10::Device dev) { return at::detail::empty_cuda(shape, dtype, dev, std::nullopt); }
+
+// elements first .. first + n - 1 of a dense vector, as a vector that shares its memory
+at::Tensor piece(const at::Tensor &t, int64_t first, int64_t n) {
+  at::Tensor v = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(t.storage()), t.key_set(), t.dtype());
+  c10::TensorImpl *impl = v.unsafeGetTensorImpl();
+  impl->set_version_counter(t.unsafeGetTensorImpl()->version_counter());   // (without one it could not be changed in place)
+  impl->set_storage_offset(first);
+  impl->set_sizes_contiguous({n});
+  return v;
+}
+
+void arguments(Py_ssize_t got, Py_ssize_t want) {
+  if (got == want) return;
+  PyErr_Format(PyExc_TypeError, "%zd arguments, not %zd", want, got);
+  throw python_error();
+}
+
+// ctx_lens, new_lens, block_table, page_size, max_tokens, free_pages, free_head -> slots, positions, cu_new, lens, info
+PyObject *page_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arguments(n, 7);
+  const at::Tensor &ctx = tensor(a[0], "ctx_lens"), &add = tensor(a[1], "new_lens"), &table = tensor(a[2], "block_table");
+  const int page = int32(a[3], "page_size"), most = int32(a[4], "max_tokens");
+  const c10::Device dev = ctx.device();
+  const int64_t B = ctx.numel();
+  if (!ctx.is_cuda() || table.dim() != 2 || table.size(0) != B || add.numel() != B || most < 0)
+    refuse("ctx_lens, new_lens [B] and block_table [B, max_pages] must be cuda tensors of one batch, max_tokens >= 0");
+  const void *pc = dense("ctx_lens", ctx, at::kInt, dev), *pn = dense("new_lens", add, at::kInt, dev);
+  void *pt = dense("block_table", table, at::kInt, dev);
+  const void *pf = nullptr, *ph = nullptr;
+  int64_t nf = 0;
+  if (a[5] != Py_None) {
+    const at::Tensor &t = tensor(a[5], "free_pages");
+    pf = dense("free_pages", t, at::kInt, dev);
+    nf = t.numel();
+    if (!pf) pf = pc;   // (an empty list has no address, but is not the absence of a list: any other address stands in for it)
+  }
+  if (a[6] != Py_None) {
+    const at::Tensor &t = tensor(a[6], "free_head");
+    if (t.numel() != 1) refuse("free_head must be one int32");
+    ph = dense("free_head", t, at::kInt, dev);
+  }
+  const c10::cuda::CUDAGuard guard(dev);
+  // the int32 results are pieces of one allocation
+  const int64_t at[5] = {0, most, most + B + 1, most + 2 * B + 1, most + 2 * B + 3};
+  at::Tensor res[5] = {empty({most}, at::kLong, dev)};
+  const at::Tensor ints = empty({at[4]}, at::kInt, dev);
+  int32_t *pi = (int32_t *)ints.data_ptr();
+  check(snlp_page_plan((const int32_t *)pc, (const int32_t *)pn, int32(B, "B"), page, (const int32_t *)pf, int32(nf, "n_free"), (const int32_t *)ph, (int32_t *)pt,
+                       int32(table.size(1), "max_pages"), most, (int64_t *)res[0].data_ptr(), pi + at[0], pi + at[1], pi + at[2], pi + at[3],
+                       c10::cuda::getCurrentCUDAStream(dev.index()).stream()));
+  for (int i = 0; i < 4; ++i) res[1 + i] = piece(ints, at[i], at[i + 1] - at[i]);
+  PyObject *out = PyTuple_New(5);
+  if (!out) throw python_error();
+  for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(out, i, THPVariable_Wrap(std::move(res[i])));
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+void rows(bool write, const at::Tensor &pool, const at::Tensor &k, const at::Tensor &v, const at::Tensor &slots) {
+  const snlp_kv4_pool p = pool_of(pool);
+  const c10::Device dev = pool.device();
+  const int64_t n = slots.numel();
+  auto fits = [&](const at::Tensor &t) {
+    return t.dim() == 3 && t.size(0) == n && t.size(1) == p.n_kv_head && t.size(2) == p.head_dim && t.device() == dev && t.scalar_type() == k.scalar_type() &&
+           (t.stride(2) == 1 || t.numel() == 0);
+  };
+  if (!fits(k) || !fits(v)) {
+    char msg[224];
+    snprintf(msg, sizeof msg,
+             "k and v must be [%lld, %d, %d] ([tokens, heads, head_dim], one slot per token) of one dtype on the pool's device, features contiguous", (long long)n,
+             p.n_kv_head, p.head_dim);
+    refuse(msg);
+  }
+  const int dt = dtype_of(k.scalar_type()), n32 = int32(n, "tokens");
+  const void *ps = dense("slots", slots, at::kLong, dev);
+  const bool plain = k.is_contiguous() && v.is_contiguous();
+  const int64_t strides[4] = {k.stride(0), k.stride(1), v.stride(0), v.stride(1)};
+  const c10::cuda::CUDAGuard guard(dev);
+  void *stream = c10::cuda::getCurrentCUDAStream(dev.index()).stream();
+  check(write ? snlp_kv4_write(&p, k.data_ptr(), v.data_ptr(), dt, plain ? nullptr : strides, (const int64_t *)ps, n32, stream)
+              : snlp_kv4_read(&p, k.data_ptr(), v.data_ptr(), dt, plain ? nullptr : strides, (const int64_t *)ps, n32, stream));
+}
+
+// pool, k, v, slots
+PyObject *kv4_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arguments(n, 4);
+  rows(true, tensor(a[0], "pool"), tensor(a[1], "k"), tensor(a[2], "v"), tensor(a[3], "slots"));
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// pool, slots, head_dim, dtype, k, v -> (k, v)
+PyObject *kv4_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arguments(n, 6);
+  const at::Tensor &pool = tensor(a[0], "pool"), &slots = tensor(a[1], "slots");
+  const int64_t dim = integer(a[2]);
+  if (!THPDtype_Check(a[3])) {
+    PyErr_Format(PyExc_TypeError, "dtype must be a torch.dtype, not %s", Py_TYPE(a[3])->tp_name);
+    throw python_error();
+  }
+  const snlp_kv4_pool p = pool_of(pool);
+  if (dim != p.head_dim) refuse("head_dim is not the pool's");
+  const at::ScalarType dt = reinterpret_cast<THPDtype *>(a[3])->scalar_type;
+  const c10::cuda::CUDAGuard guard(pool.device());
+  at::Tensor kv[2];
+  for (int i = 0; i < 2; ++i) {
+    if (a[4 + i] != Py_None) {
+      kv[i] = tensor(a[4 + i], i ? "v" : "k");
+    } else {
+      const PyObject *other = a[5 - i];   // of the given one's dtype
+      const at::ScalarType t = other != Py_None ? tensor(a[5 - i], i ? "k" : "v").scalar_type() : dt;
+      dtype_of(t);
+      kv[i] = empty({slots.numel(), p.n_kv_head, p.head_dim}, t, pool.device());
+    }
+  }
+  rows(false, pool, kv[0], kv[1], slots);
+  PyObject *out = PyTuple_New(2);
+  if (!out) throw python_error();
+  for (int i = 0; i < 2; ++i) {
+    if (a[4 + i] != Py_None) {
+      Py_INCREF(a[4 + i]);
+      PyTuple_SET_ITEM(out, i, a[4 + i]);
+    } else {
+      PyTuple_SET_ITEM(out, i, THPVariable_Wrap(std::move(kv[i])));
+    }
+  }
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+// q, pool, block_table, lens, cu_q, max_len, scale, out, workspace, tile_rows -> out
+PyObject *kv4_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arguments(n, 10);
+  const at::Tensor &q = tensor(a[0], "q"), &pool = tensor(a[1], "pool"), &table = tensor(a[2], "block_table"), &lens = tensor(a[3], "lens");
+  const snlp_kv4_pool p = pool_of(pool);
+  const c10::Device dev = pool.device();
+  const int64_t B = lens.numel();
+  if (q.device() != dev || q.dim() != 3 || q.size(2) != p.head_dim || (q.numel() && q.stride(2) != 1))
+    refuse("q must be [rows, n_head, head_dim] on the pool's device, features contiguous");
+  snlp_kv4_attn at{};
+  if (table.dim() != 2 || table.size(0) != B) refuse("block_table must be [B, max_pages], lens [B]");
+  if (a[4] != Py_None) {
+    const at::Tensor &cu = tensor(a[4], "cu_q");
+    if (cu.numel() != B + 1) refuse("cu_q must be [B + 1]");
+    at.cu_q = (const int32_t *)dense("cu_q", cu, at::kInt, dev);
+  }
+  at.max_len = int32(a[5], "max_len");
+  if (a[6] != Py_None) {
+    at.scale = (float)PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) throw python_error();
+    if (at.scale == 0.f) refuse("scale must not be 0");
+  }
+  at.q = q.data_ptr(); at.q_token_stride = q.stride(0); at.q_head_stride = q.stride(1);
+  at.block_table = (const int32_t *)dense("block_table", table, at::kInt, dev);
+  at.lens = (const int32_t *)dense("lens", lens, at::kInt, dev);
+  at.dtype = dtype_of(q.scalar_type()); at.n_rows = int32(q.size(0), "rows"); at.B = int32(B, "B"); at.n_head = int32(q.size(1), "n_head");
+  at.max_pages = int32(table.size(1), "max_pages"); at.tile_rows = int32(a[9], "tile_rows");
+  const c10::cuda::CUDAGuard guard(dev);
+  at::Tensor out, ws;
+  if (a[7] != Py_None) {
+    out = tensor(a[7], "out");
+    if (out.sizes() != q.sizes()) refuse("out must have q's shape");
+  } else {
+    out = empty(q.sizes(), q.scalar_type(), dev);
+  }
+  void *po = dense("out", out, q.scalar_type(), dev), *pw = nullptr;
+  size_t size = 0;
+  if (a[8] != Py_None) {
+    const at::Tensor &w = tensor(a[8], "workspace");
+    pw = dense("workspace", w, at::kByte, dev);
+    size = (size_t)w.numel();
+  } else {
+    check(snlp_kv4_attention_workspace(&p, &at, &size));
+    if (size) {
+      ws = empty({(int64_t)size}, at::kByte, dev);
+      pw = ws.data_ptr();
+    }
+  }
+  check(snlp_kv4_attention(&p, &at, po, pw, size, c10::cuda::getCurrentCUDAStream(dev.index()).stream()));
+  if (a[7] != Py_None) {
+    Py_INCREF(a[7]);
+    return a[7];
+  }
+  return THPVariable_Wrap(std::move(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// refuse, check: see above; returns the torch version this module was built with
+PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  arguments(n, 2);
+  Py_INCREF(a[0]);
+  Py_INCREF(a[1]);
+  Py_XDECREF(g_refuse);
+  Py_XDECREF(g_check);
+  g_refuse = a[0];
+  g_check = a[1];
+  return PyUnicode_FromString(TORCH_VERSION);
+  END_HANDLE_TH_ERRORS
+}
+
+#define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {ENTRY(bind), ENTRY(page_plan), ENTRY(kv4_write), ENTRY(kv4_read), ENTRY(kv4_attention), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__bind() { return PyModule_Create(&module); }

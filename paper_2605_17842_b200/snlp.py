@@ -1,6 +1,7 @@
-"""Thin ctypes binding over libsnlp.so (argument marshalling only; every step runs in the CUDA library).
+"""Thin binding over libsnlp.so (argument marshalling only; every step runs in the CUDA library): ctypes, and for the operators
+of a layer or step, whose kernels take a few microseconds, the native _bind.so.
 
-Importing this module loads the library and raises if it is missing: there is no fallback path.
+Importing this module loads both and raises if one is missing: there is no fallback path.
 Device memory is held in torch tensors; the current torch CUDA stream is passed to every call.
 """
 from __future__ import annotations
@@ -333,9 +334,7 @@ def lm_head_greedy_static(hL: torch.Tensor, lm_head_bf16: torch.Tensor, n_stream
 
 # -- key/value cache held in 4 bits ------------------------------------------------------------------
 KV4_BLOCK = 16                                   # tokens of a storage block
-KV4_MIN_SPLIT = 128                              # keys of the shortest split of the attention
 _KV4_BLOCK_BYTES = {64: 1152, 128: 2304}         # by head_dim: 16 tokens' codes and parameters, keys and values
-_KV4_HEAD_DIM = {v: k for k, v in _KV4_BLOCK_BYTES.items()}
 
 
 class PagePlan(NamedTuple):
@@ -351,32 +350,17 @@ def _refuse(msg):
     raise SnlpError(ERR_ARG, msg)
 
 
-_I, _V, _Z = C.c_int, C.c_void_p, C.c_size_t
-_lib.snlp_page_plan.argtypes = [_V, _V, _I, _I, _V, _I, _V, _V, _I, _I, _V, _V, _V, _V, _V, _V]
-_lib.snlp_kv4_write.argtypes = [_V, _V, _V, _I, _V, _V, _I, _V]
-_lib.snlp_kv4_read.argtypes = _lib.snlp_kv4_write.argtypes
-_lib.snlp_kv4_attention_workspace.argtypes = [_V, _V, _V]
-_lib.snlp_kv4_attention.argtypes = [_V, _V, _V, _V, _Z, _V]
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-_Strides = C.c_int64 * 4
-_INT_MAX = 0x7fffffff
+def _load_bind(path: str = os.path.join(_HERE, "_bind.so")):
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is missing: build it with `python -m paper_2605_17842_b200.build`")
+    from . import _bind
+    built = _bind.bind(_refuse, _check)
+    if built.split("+")[0] != torch.__version__.split("+")[0]:
+        raise ImportError(f"{path} was built with torch {built}, this is {torch.__version__}: build it again with `python -m paper_2605_17842_b200.build --force`")
+    return _bind
 
 
-def _call_on(index, fn, *args):
-    """fn(*args, stream) with the tensors' device current, on that device's current stream."""
-    if _current_device() == index:
-        rc = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
-            rc = fn(*args, _raw_stream(index))
-    if rc:
-        _check(rc)
-
-
-def _dense_ptr(what, t, dtype, dev):
-    if t.dtype is not dtype or t.device != dev or not t.is_contiguous():
-        _refuse(f"{what} must be a contiguous {dtype} tensor on {dev}")
-    return t.data_ptr()
+_bind = _load_bind()
 
 
 def kv4_pool(n_pages: int, n_kv_head: int, head_dim: int, page_size: int, device="cuda") -> torch.Tensor:
@@ -387,76 +371,24 @@ def kv4_pool(n_pages: int, n_kv_head: int, head_dim: int, page_size: int, device
     return torch.empty((n_pages, n_kv_head, page_size // KV4_BLOCK, _KV4_BLOCK_BYTES[head_dim]), dtype=torch.uint8, device=device)
 
 
-def _kv4_pool_arg(pool):
-    shape = pool.shape
-    if pool.dtype is not torch.uint8 or not pool.is_cuda or len(shape) != 4 or not pool.is_contiguous() or shape[3] not in _KV4_HEAD_DIM:
-        _refuse("pool must be a contiguous cuda uint8 tensor shaped as kv4_pool makes it")
-    n, h, b, size = shape
-    return Kv4Pool(pool.data_ptr(), n, b * KV4_BLOCK, h, _KV4_HEAD_DIM[size])
-
-
-_KV4_DTYPE = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32}
-
-
-def _kv4_dtype(t):
-    if t not in _KV4_DTYPE:
-        _refuse("keys, values and queries are bfloat16 or float32")
-    return _KV4_DTYPE[t]
-
-
 def page_plan(ctx_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor, page_size: int, max_tokens: int,
               free_pages: torch.Tensor | None = None, free_head: torch.Tensor | None = None) -> PagePlan:
     """Block tables and slot maps from request lengths (snlp_page_plan): int32 cuda tensors ctx_lens, new_lens [B];
     block_table [B, max_pages] is completed in place with pages from free_pages[free_head:] (None: it has them all).
     max_tokens: length of the slot map, at least the number of new tokens."""
-    dev, B, shape, i32 = ctx_lens.device, ctx_lens.numel(), block_table.shape, torch.int32
-    if not ctx_lens.is_cuda or len(shape) != 2 or shape[0] != B or new_lens.numel() != B or not 0 <= max_tokens <= _INT_MAX:
-        _refuse("ctx_lens, new_lens [B] and block_table [B, max_pages] must be cuda tensors of one batch, max_tokens >= 0 and an int32")
-    if free_head is not None and free_head.numel() != 1:
-        _refuse("free_head must be one int32")
-    pc, pn, pt = _dense_ptr("ctx_lens", ctx_lens, i32, dev), _dense_ptr("new_lens", new_lens, i32, dev), _dense_ptr("block_table", block_table, i32, dev)
-    # (an empty list has no address, but is not the absence of a list: any other address stands in for it)
-    pf, nf = (_dense_ptr("free_pages", free_pages, i32, dev) or pc, free_pages.numel()) if free_pages is not None else (None, 0)
-    ph = _dense_ptr("free_head", free_head, i32, dev) if free_head is not None else None
-    slots = ctx_lens.new_empty(max_tokens, dtype=torch.int64)
-    ints = ctx_lens.new_empty(max_tokens + 2 * B + 3)     # the int32 results, in one piece
-    at = ints.data_ptr()
-    positions, cu, lens, info = at, at + 4 * max_tokens, at + 4 * (max_tokens + B + 1), at + 4 * (max_tokens + 2 * B + 1)
-    _call_on(dev.index, _lib.snlp_page_plan, pc, pn, B, page_size, pf, nf, ph, pt, shape[1], max_tokens, slots.data_ptr(), positions, cu, lens, info)
-    return PagePlan(slots, *ints.split_with_sizes((max_tokens, B + 1, B, 2)))
-
-
-def _kv4_rows(fn, pool, k, v, slots):
-    p, dev, n, dt = _kv4_pool_arg(pool), pool.device, slots.numel(), k.dtype
-    if n > _INT_MAX:
-        _refuse("more than 2^31 - 1 tokens in one call")
-    shape = (n, p.n_kv_head, p.head_dim)
-    strides = None                               # dense
-    ok = k.shape == shape and v.shape == shape and k.device == dev and v.device == dev and v.dtype is dt
-    if ok and not (k.is_contiguous() and v.is_contiguous()):
-        (kt, kh, ke), (vt, vh, ve) = k.stride(), v.stride()
-        ok, strides = ke == 1 and ve == 1, _Strides(kt, kh, vt, vh)
-    if not ok:
-        _refuse(f"k and v must be {list(shape)} ([tokens, heads, head_dim], one slot per token) of one dtype on the pool's device, features contiguous")
-    _call_on(dev.index, fn, C.byref(p), k.data_ptr(), v.data_ptr(), _kv4_dtype(dt), strides,
-             _dense_ptr("slots", slots, torch.int64, dev), n)
+    return PagePlan._make(_bind.page_plan(ctx_lens, new_lens, block_table, page_size, max_tokens, free_pages, free_head))
 
 
 def kv4_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Store k, v [n, n_kv_head, head_dim] (bf16 or fp32, any token and head stride) at int64 slots [n]; tokens whose slot
     lies outside the pool are left out."""
-    _kv4_rows(_lib.snlp_kv4_write, pool, k, v, slots)
+    _bind.kv4_write(pool, k, v, slots)
 
 
 def kv4_read(pool: torch.Tensor, slots: torch.Tensor, head_dim: int, dtype=torch.bfloat16, k: torch.Tensor | None = None,
              v: torch.Tensor | None = None):
     """(k, v) [n, n_kv_head, head_dim] of the tokens at int64 slots [n]; zeros where a slot lies outside the pool."""
-    if k is None or v is None:
-        shape = (slots.numel(), pool.shape[1], head_dim)
-        k = pool.new_empty(shape, dtype=dtype) if k is None else k
-        v = torch.empty_like(k) if v is None and k.is_contiguous() else pool.new_empty(shape, dtype=dtype) if v is None else v
-    _kv4_rows(_lib.snlp_kv4_read, pool, k, v, slots)
-    return k, v
+    return _bind.kv4_read(pool, slots, head_dim, dtype, k, v)
 
 
 def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor | None = None,
@@ -466,39 +398,7 @@ def kv4_attention(q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor
     lens [B]; cu_q [B + 1] gives each sequence's rows (None: rows / B each).  max_len: a bound of the lengths known on the
     host (0: the table's capacity); workspace: uint8, by default allocated per call; tile_rows: 2, 4, 8 or 16 rows worked on
     together (0: chosen by the sizes), one value for calls whose rows have to agree bit for bit."""
-    p, dev, shape, B, tab, i32 = _kv4_pool_arg(pool), pool.device, q.shape, lens.numel(), block_table.shape, torch.int32
-    if q.device != dev or len(shape) != 3 or shape[2] != p.head_dim or (shape[0] and q.stride(2) != 1):
-        _refuse("q must be [rows, n_head, head_dim] on the pool's device, features contiguous")
-    if len(tab) != 2 or tab[0] != B or (cu_q is not None and cu_q.numel() != B + 1):
-        _refuse("block_table must be [B, max_pages], lens [B], cu_q [B + 1]")
-    if not 0 <= max_len <= _INT_MAX or scale == 0:
-        _refuse("max_len must be 0 .. 2^31 - 1, scale not 0")
-    if out is None:
-        out = torch.empty_like(q) if q.is_contiguous() else torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif out.shape != shape:
-        _refuse("out must have q's shape")
-    qt, qh, _ = q.stride()
-    a = Kv4Attn(q.data_ptr(), qt, qh, _dense_ptr("block_table", block_table, i32, dev), _dense_ptr("lens", lens, i32, dev),
-                _dense_ptr("cu_q", cu_q, i32, dev) if cu_q is not None else None, _kv4_dtype(q.dtype), shape[0], B, shape[1], tab[1], max_len,
-                tile_rows, scale if scale is not None else 0.0)
-    po = _dense_ptr("out", out, q.dtype, dev)
-    pp, pa, pw, size = C.byref(p), C.byref(a), None, 0
-    if workspace is None:
-        # no split is shorter than KV4_MIN_SPLIT keys: where that bound is small, it does without the question
-        keys = tab[1] * p.page_size
-        splits = -(-(min(max_len, keys) if max_len > 0 else keys) // KV4_MIN_SPLIT)
-        size = shape[0] * shape[1] * splits * (p.head_dim + 4) * 4 if splits > 1 else 0
-        if size > 1 << 22:
-            need = C.c_size_t()
-            _check(_lib.snlp_kv4_attention_workspace(pp, pa, C.byref(need)))
-            size = need.value
-        if size:
-            workspace = pool.new_empty(size)
-            pw = workspace.data_ptr()
-    else:
-        pw, size = _dense_ptr("workspace", workspace, torch.uint8, dev), workspace.numel()
-    _call_on(dev.index, _lib.snlp_kv4_attention, pp, pa, po, pw, size)
-    return out
+    return _bind.kv4_attention(q, pool, block_table, lens, cu_q, max_len, scale, out, workspace, tile_rows)
 
 
 def raw_library() -> C.CDLL:

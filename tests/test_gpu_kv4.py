@@ -115,6 +115,45 @@ def test_bindings_refuse_what_ctypes_would_cut(S):
             f()
 
 
+def test_results_are_ordinary_tensors(S):
+    """What the binding allocates can be changed in place, sliced, saved by autograd and freed in any order; pieces of one
+    allocation do not reach into each other."""
+    n, pool = torch.ones(3, dtype=torch.int32, device="cuda"), S.kv4_pool(3, 2, 64, 16)
+    for mode in (torch.no_grad, torch.enable_grad, torch.inference_mode):
+        with mode():
+            table = torch.arange(3, dtype=torch.int32, device="cuda").reshape(3, 1)
+            plan = S.page_plan(n * 0, n, table, 16, 4)
+            assert [t.tolist() for t in plan] == [[0, 16, 32, -1], [0, 0, 0, -1], [0, 1, 2, 3], [1, 1, 1], [0, 0]]
+            assert all(t.is_contiguous() and t.device == pool.device for t in plan)
+            for i, t in enumerate(plan):
+                before = [u.clone() for u in plan]
+                t.add_(5)
+                t[:1].zero_()
+                assert t[0] == 0 and torch.equal(t[1:], before[i][1:] + 5)
+                assert all(torch.equal(u, before[j]) for j, u in enumerate(plan) if j != i)
+            keep = plan.lens.clone(), plan.lens
+            del plan, t, before
+            torch.empty(4096, dtype=torch.int32, device="cuda").fill_(9)
+            assert torch.equal(*keep)
+            k, v = S.kv4_read(pool.fill_(0), torch.arange(5, device="cuda"), 64)
+            k.add_(1)
+            assert (k == 1).all() and (v == 0).all()
+            out = S.kv4_attention(k[:3], pool, table, n, max_len=16)
+            assert (out.sub_(1) == -1).all()
+    w = torch.ones(2, device="cuda", requires_grad=True)
+    k, _ = S.kv4_read(pool.fill_(0), torch.arange(5, device="cuda"), 64, torch.float32)
+    (w[0] * (k + 1)).sum().backward()
+    assert w.grad.tolist() == [5 * 2 * 64, 0]
+
+
+def test_bindings_name_what_is_not_a_tensor(S):
+    pool, n = S.kv4_pool(3, 2, 64, 16), torch.ones(3, dtype=torch.int32, device="cuda")
+    for f in (lambda: S.kv4_write(pool, None, None, n), lambda: S.kv4_read(pool, n.long(), 64, "bf16"), lambda: S.page_plan([1], n, n, 16, 3),
+              lambda: S.kv4_attention(1.0, pool, n, n)):
+        with pytest.raises(TypeError):
+            f()
+
+
 def test_plan_full_table_takes_nothing(S):
     table = np.arange(12, dtype=np.int32).reshape(3, 4)
     table[1, 2] = -1                                    # a hole: its tokens have no slot
