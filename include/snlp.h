@@ -358,8 +358,8 @@ int snlp_kv4_read(const snlp_kv4_pool *pool, void *k, void *v, int dtype, const 
  * out [n_rows][n_head][head_dim], q's dtype, dense, not overlapping q.  bf16 results: probabilities are rounded to 11 bits before the second
  * product; fp32 results: queries and probabilities are split in two such terms (22 bits); all sums are fp32.
  *   tile_rows  query rows of a sequence and key/value head that are worked on together, 2, 4, 8 or 16; 0 = the smallest that
- *         holds the average.  For one tile_rows a row's result depends on its own query, its visible keys, B * n_kv_head and
- *         max_len only, bit for bit: a caller who wants single tokens and verify blocks to agree gives both the same.
+ *         holds the average.  For one tile_rows (not 0) a row's result depends on its own query, its visible keys, B * n_kv_head
+ *         and max_len only, bit for bit: a caller who wants single tokens and verify blocks to agree gives both the same.
  * workspace (device, 16-byte aligned, snlp_kv4_attention_workspace bytes, may be NULL if that is 0) needs no initial
  * contents; calls that may overlap on the GPU need one each.
  * Errors: ARG, SHAPE (B > 4096, too many rows), UNSUPPORTED (head_dim), CUDA. */

@@ -74,24 +74,51 @@ static cudaError_t rows_launch(const Kv4Rows &p, cudaStream_t st) {
 cudaError_t kv4_write(const Kv4Rows &p, cudaStream_t st) { return rows_launch<true>(p, st); }
 cudaError_t kv4_read(const Kv4Rows &p, cudaStream_t st) { return rows_launch<false>(p, st); }
 
-// Keys of a split, as a power of two: it depends on the number of (sequence, key/value head) pairs and the longest length allowed
-// only -- not on the lengths, query rows or layers of a call -- so that calls on one cache merge a row's keys in the same order.
-// Few pairs: short splits, many warps; many pairs: long ones, which cost less to begin and to end; and at most 256 of them.
-static int chunk_shift(int pairs, int max_len) {
-  int sh = pairs < 32 ? 7 : pairs < 256 ? 8 : 9;
-  while (((int64_t)max_len >> sh) > 256 && sh < 11) ++sh;
-  return sh;
+// Tile: the smallest that holds the rows which a sequence brings to a key/value head, on average.
+// Split: a warp takes 64 keys in 2 .. 4 us, so splits are short while there are too few of them for the warps of the GPU (12 an SM in bf16
+// with tiles up to 8 rows, else 8), and long where there are many: each costs a beginning, an end and a row of partial results.
+// It follows from sizes of the call, never from lengths, and with a tile that the caller chose not from the number of rows
+// either: calls that share tile, pairs (sequences x key/value heads) and longest length merge a row's keys in the same order.
+static int longer_where_many(int split, int max_len) {   // at most 256 splits, as far as 2048 keys go
+  while (((int64_t)max_len >> split) > 256 && split < 11) ++split;
+  return split;
 }
 
-static int chunks_max(int B, int Hkv, int max_len) {
-  const int sh = chunk_shift(B * Hkv, max_len);
-  return (int)(((int64_t)max_len + (1 << sh) - 1) >> sh);
+Kv4Shape kv4_shape(int n_rows, int B, int Hq, int Hkv, int max_len, int tile_rows, bool fp32) {
+  const int64_t G = Hq / Hkv, pairs = (int64_t)B * Hkv, rows = ((int64_t)n_rows * G + B - 1) / B;
+  const int tile = tile_rows ? tile_rows : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  if (max_len <= 128) return {tile, 7};   // in one go, nothing to join
+  int sh;
+  if (tile < 16) {
+    // The shortest split that does not give more units than there are warps, 512 keys at the most.  64 / 128 / 256 / 512 keys, one token a
+    // sequence, bf16, us: 10 pairs x 2048 keys 9.5 / 10.2 / 12.0 / 15.9, x 32768 29.2 / 24.6 / 20.5 / 27.1, 80 pairs x 2048
+    // 15.0 / 13.4 / 17.7 / 26.3, 128 x 4096 34.1 / 31.0 / 32.9 / 29.9, 256 x 8192 118 / 92 / 75 / 74.
+    const int64_t most = fp32 ? 1184 : 1776;
+    sh = 6;
+    while (sh < 9 && pairs * (((int64_t)max_len + (1 << sh) - 1) >> sh) > most) ++sh;
+  } else if (tile_rows) {
+    sh = 9;
+  } else {
+    // Many rows a sequence: the longest split that leaves enough units.  128 / 256 / 512 / 1024 keys, us: 10 heads x 40 rows x 4096 keys
+    // 20 / 25 / 38 / 47; 36 pairs x 200 rows x 3000 147 / 107 / 104 / 117; 8 x 800 x 3000 134 / 112 / 98 / 114; 64 x 256 x 2048
+    // 213 / 154 / 143 / 127.  (10 heads x 9 rows x 4105 keys: 64 / 128 keys 14.8 / 17.1.)
+    const int64_t tiles = Hkv * (((int64_t)n_rows * G + 15) / 16);
+    auto units = [&](int s) { return tiles * (((int64_t)max_len + (1 << s) - 1) >> s); };
+    sh = units(10) >= 2000 ? 10 : units(9) >= 1000 ? 9 : units(8) >= 1000 ? 8 : units(7) >= 500 ? 7 : 6;
+  }
+  return {tile, longer_where_many(sh, max_len)};
 }
 
-int kv4_attention_launches(int B, int Hkv, int max_len) { return chunks_max(B, Hkv, max_len) > 1 ? 2 : 1; }
+// A model's sweeps run all layers in one launch, its layer-by-layer steps one: their splits have to agree and are chosen for the sweeps.
+// One tile for single tokens and blocks of them, so that a verify block reproduces the decode steps bit for bit.
+Kv4Shape kv4_shape_model(int pairs, int max_len) { return {2, longer_where_many(pairs < 32 ? 7 : pairs < 256 ? 8 : 9, max_len)}; }
 
-size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl) {
-  const int n = chunks_max(B, Hkv, max_len);
+static int splits_max(int max_len, int split) { return (int)(((int64_t)max_len + (1 << split) - 1) >> split); }
+
+int kv4_attention_launches(int max_len, int split) { return splits_max(max_len, split) > 1 ? 2 : 1; }
+
+size_t kv4_workspace(int n_rows, int Hq, int hd, int max_len, int split, int nl) {
+  const int n = splits_max(max_len, split);
   return n < 2 ? 0 : (size_t)nl * n_rows * Hq * n * (hd + 4) * sizeof(float);
 }
 
@@ -160,16 +187,13 @@ cudaError_t kv4_attention(const Kv4Attn &a, int n_sm, cudaStream_t st) {
   Attn4Params p{};
   p.a = a;
   p.G = a.Hq / a.Hkv;
-  p.chunk_sh = chunk_shift(a.B * a.Hkv, a.max_len);
-  p.nch_max = std::max(1, chunks_max(a.B, a.Hkv, a.max_len));
+  p.chunk_sh = a.split;
+  p.nch_max = std::max(1, splits_max(a.max_len, a.split));
   p.qk_scale = a.scale * 1.4426950408889634f;
   const size_t u = a.fp32 ? 4 : 8;
   p.vec = (uintptr_t)a.q % 16 == 0 && a.q_ls % u == 0 && a.q_ts % u == 0 && a.q_hs % u == 0 ? 16 : 0;
-  // rows that a sequence brings to a key/value head, on average: the smallest tile that holds them
-  const int64_t rows = ((int64_t)a.n_rows * p.G + a.B - 1) / a.B;
-  const int tile = a.tile ? a.tile : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-  if (a.fp32) return a.hd == 128 ? attn_pick<float, 128>(p, tile, n_sm, st) : attn_pick<float, 64>(p, tile, n_sm, st);
-  return a.hd == 128 ? attn_pick<__nv_bfloat16, 128>(p, tile, n_sm, st) : attn_pick<__nv_bfloat16, 64>(p, tile, n_sm, st);
+  if (a.fp32) return a.hd == 128 ? attn_pick<float, 128>(p, a.tile, n_sm, st) : attn_pick<float, 64>(p, a.tile, n_sm, st);
+  return a.hd == 128 ? attn_pick<__nv_bfloat16, 128>(p, a.tile, n_sm, st) : attn_pick<__nv_bfloat16, 64>(p, a.tile, n_sm, st);
 }
 
 }  // namespace snlp
@@ -297,6 +321,10 @@ static int attn_check(const snlp_kv4_attn *a, const snlp_kv4_pool *pool, const c
   return SNLP_OK;
 }
 
+static Kv4Shape attn_shape(const snlp_kv4_attn *a, const snlp_kv4_pool *pool, int max_len) {
+  return kv4_shape(a->n_rows, a->B, a->n_head, pool->n_kv_head, max_len, a->tile_rows, a->dtype == SNLP_DTYPE_FP32);
+}
+
 static int attn_max_len(const snlp_kv4_attn *a, const snlp_kv4_pool *pool) {
   const int cap = a->max_pages * pool->page_size;
   return a->max_len > 0 && a->max_len < cap ? a->max_len : cap;
@@ -309,7 +337,8 @@ extern "C" int snlp_kv4_attention_workspace(const snlp_kv4_pool *pool, const snl
   p.pages = (void *)16;   // not looked at
   int rc = check_pool(&p, who);
   if (rc != SNLP_OK || (rc = attn_check(args, pool, who)) != SNLP_OK) return rc;
-  *bytes = kv4_workspace(args->n_rows, args->B, args->n_head, pool->n_kv_head, pool->head_dim, attn_max_len(args, pool), 1);
+  const int max_len = attn_max_len(args, pool);
+  *bytes = kv4_workspace(args->n_rows, args->n_head, pool->head_dim, max_len, attn_shape(args, pool, max_len).split, 1);
   return SNLP_OK;
 }
 
@@ -326,11 +355,12 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   if (!std::isfinite(args->scale)) return refuse(SNLP_ERR_ARG, "%s: scale is not a finite number", who);
   Kv4Attn a{};
   a.max_len = attn_max_len(args, pool);
-  const size_t need = kv4_workspace(args->n_rows, args->B, args->n_head, pool->n_kv_head, pool->head_dim, a.max_len, 1);
+  const Kv4Shape shape = attn_shape(args, pool, a.max_len);
+  const size_t need = kv4_workspace(args->n_rows, args->n_head, pool->head_dim, a.max_len, shape.split, 1);
   if (need > 0 && (!workspace || workspace_bytes < need)) return refuse(SNLP_ERR_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : (size_t)0, need);
   if ((uintptr_t)workspace % 16) return refuse(SNLP_ERR_ARG, "%s: the workspace must be 16-byte aligned", who);
   const int64_t G = args->n_head / pool->n_kv_head;
-  const int64_t units = (args->n_rows * G / 2 + args->B) * (int64_t)(((int64_t)a.max_len + 127) / 128);
+  const int64_t units = (args->n_rows * G / 2 + args->B) * (int64_t)(((int64_t)a.max_len + 63) / 64);
   if (units > 0x7fffffffLL || (int64_t)args->n_rows * args->n_head > 0x7fffffffLL) return refuse(SNLP_ERR_SHAPE, "%s: too many rows in one call", who);
   if ((rc = launched(kv4_init(), who)) != SNLP_OK) return rc;
   int dev = 0, n_sm = 0;
@@ -341,7 +371,7 @@ extern "C" int snlp_kv4_attention(const snlp_kv4_pool *pool, const snlp_kv4_attn
   a.pool = (const uint8_t *)pool->pages; a.table = args->block_table; a.tstride = args->max_pages; a.lens = args->lens; a.cu = args->cu_q;
   a.out = out; a.part = (float *)workspace;
   a.T = args->n_rows / args->B; a.n_rows = args->n_rows; a.B = args->B; a.Hq = args->n_head; a.Hkv = pool->n_kv_head; a.hd = pool->head_dim;
-  a.n_pages = pool->n_pages; a.page = pool->page_size; a.nl = 1; a.tile = args->tile_rows; a.fp32 = args->dtype == SNLP_DTYPE_FP32;
+  a.n_pages = pool->n_pages; a.page = pool->page_size; a.nl = 1; a.tile = shape.tile; a.split = shape.split; a.fp32 = args->dtype == SNLP_DTYPE_FP32;
   a.scale = args->scale != 0.f ? args->scale : (pool->head_dim == 128 ? 0.08838834764831845f : 0.125f);
   return launched(kv4_attention(a, n_sm, (cudaStream_t)stream), who);
 }

@@ -575,9 +575,9 @@ static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, int
 // prefix sum over the lengths), of which its four warps take the next one as they come (dealt out beforehand, the warps with
 // a unit more than others ran alone at the end: 94 us for the last of 160 x 10 heads x 2048 keys where the median was 76), each
 // with a ring of cp.async stages of its own that runs on across units: after the prefix sum no warp waits for another.  A
-// warp joins its columns at the end of a unit; rows with several chunks are joined by k_kv4_merge in chunk order.  The chunk length depends on the number of (sequence, head) pairs and the longest length allowed,
-// and a row's arithmetic on its own visible keys and RW, so for one RW a row comes out the same whether it is decoded alone,
-// in a verify block or in a sweep over all layers.
+// warp joins its columns at the end of a unit; rows with several chunks are joined by k_kv4_merge in chunk order.  The chunk length does not depend on the lengths, nor on the rows
+// where the caller fixes the tile (kv4.cu), and a row's arithmetic on its own visible keys and RW only, so for one RW a row
+// comes out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
 // Bound: for one row of 160 x 10 heads x 2048 keys (472 MB, 98 us with the join = 4.8 TB/s, 97 us of it here) the copies alone
 // take 84 us and the arithmetic alone 86 us; the codes' masks, shifts and byte moves keep the ALU pipe at 53 % with 12 warps
 // an SM (163 registers, 221 KB of stages).  For prompt chunks the mma.sync rate and the same unpacking: 62 TFLOP/s.

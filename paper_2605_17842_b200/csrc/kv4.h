@@ -48,14 +48,19 @@ struct Kv4Attn {
   void *out; size_t o_ls;                   // [rows][Hq][hd]
   float *part;                              // workspace
   int T, n_rows, B, Hq, Hkv, hd, n_pages, page, max_len, nl;
-  int tile;                                 // query rows of a work unit: 2, 4, 8 or 16; 0 = chosen by the rows of a sequence and kv head
+  int tile;                                 // query rows of a work unit: 2, 4, 8 or 16
+  int split;                                // keys of a split, as a power of two: 6 .. 11
   float scale;
   bool fp32;
   bool pdl;                                 // programmatic dependent launch behind the kernel before it
 };
-size_t kv4_workspace(int n_rows, int B, int Hq, int Hkv, int hd, int max_len, int nl);
+// Tile and split of a call, and of the calls on a model's cache, which all have the same (kv4.cu).
+struct Kv4Shape { int tile, split; };
+Kv4Shape kv4_shape(int n_rows, int B, int Hq, int Hkv, int max_len, int tile_rows, bool fp32);
+Kv4Shape kv4_shape_model(int pairs, int max_len);
+size_t kv4_workspace(int n_rows, int Hq, int hd, int max_len, int split, int nl);
 cudaError_t kv4_attention(const Kv4Attn &p, int n_sm, cudaStream_t st);
-int kv4_attention_launches(int B, int Hkv, int max_len);   // kernels of one call
+int kv4_attention_launches(int max_len, int split);   // kernels of one call
 cudaError_t kv4_init();                     // kernel attributes of the current device
 
 }  // namespace snlp

@@ -681,7 +681,8 @@ static int kv4_attend(snlp_model *m, const Fwd &f, int l0, int nl, const void *q
   a.T = f.T; a.n_rows = f.M; a.B = f.B; a.Hq = a.Hkv = c.n_head; a.hd = c.head_dim; a.n_pages = f.kv4->n_pages; a.page = kKv4Page;
   a.max_len = f.kv4->max_ctx; a.scale = 1.f / std::sqrt((float)c.head_dim); a.fp32 = c.dtype == SNLP_DTYPE_FP32;
   a.pdl = m->pdl_now;
-  a.tile = 2;   // one tile for single tokens and blocks of them, so that a verify block reproduces the decode steps bit for bit
+  const Kv4Shape shape = kv4_shape_model(f.B * c.n_head, a.max_len);
+  a.tile = shape.tile; a.split = shape.split;
   // the decode regime has workspace for all layers at once; more rows go layer by layer
   const bool all = f.M <= kDecodeRows;
   for (int i = 0; i < nl; i += all ? nl : 1) {
@@ -689,7 +690,7 @@ static int kv4_attend(snlp_model *m, const Fwd &f, int l0, int nl, const void *q
     a.pool = f.kv4->pool + (size_t)(l0 + i) * f.kv4->pool_ls;
     a.part = all ? m->attn_part : f.kv4->part; a.nl = all ? nl : 1;
     TimedLaunch tl_(m, f.st, KC_ATTN);
-    count(m, kv4_attention_launches(f.B, c.n_head, a.max_len) - 1);
+    count(m, kv4_attention_launches(a.max_len, a.split) - 1);
     TRY(kv4_check(kv4_attention(a, m->n_sm, f.st)));
   }
   return SNLP_OK;
@@ -1395,7 +1396,7 @@ extern "C" int snlp_kv_create_4bit(snlp_model *m, int B, int max_ctx, snlp_kv **
   const size_t pool = c.n_layer * kv->pool_ls;
   const bool prompts = m->have_wmaps && c.dtype == SNLP_DTYPE_BF16 && c.head_dim == 128;   // the tensor-core prompt attention serves this model
   const size_t dense = prompts ? (size_t)B * max_ctx * c.d_model * m->esz : 0;
-  const size_t part = kv4_workspace(c.max_rows, B, c.n_head, c.n_head, c.head_dim, max_ctx, 1);
+  const size_t part = kv4_workspace(c.max_rows, c.n_head, c.head_dim, max_ctx, kv4_shape_model(B * c.n_head, max_ctx).split, 1);
   bool ok = cudaMalloc((void **)&kv->pool, pool) == cudaSuccess && cudaMalloc((void **)&kv->table, (size_t)kv->n_pages * 4) == cudaSuccess &&
             cudaMalloc((void **)&kv->lens, (size_t)B * 4) == cudaSuccess && cudaMalloc((void **)&kv->slots, (size_t)c.max_rows * 8) == cudaSuccess &&
             cudaMalloc((void **)&kv->all_slots, (size_t)B * max_ctx * 8) == cudaSuccess && cudaMalloc((void **)&kv->pos, 16) == cudaSuccess &&

@@ -85,7 +85,7 @@ def test_attention():
     assert go(max_pages=1 << 28) == snlp.ERR_SHAPE
     assert go(n_rows=1 << 30, B=2, n_head=4) == snlp.ERR_SHAPE
     # a workspace that is missing or too small
-    assert lib.snlp_kv4_attention_workspace(C.byref(pool(pages=None)), C.byref(attn(max_pages=100)), C.byref(n)) == 0 and n.value == 2 * 4 * 13 * 68 * 4
+    assert lib.snlp_kv4_attention_workspace(C.byref(pool(pages=None)), C.byref(attn(max_pages=100)), C.byref(n)) == 0 and n.value == 2 * 4 * 25 * 68 * 4
     assert go(max_pages=100, ws=0, size=0) == snlp.ERR_ARG and str(n.value) in message()
     assert go(max_pages=100, size=n.value - 1) == snlp.ERR_ARG
     assert lib.snlp_kv4_attention_workspace(C.byref(pool(pages=None)), C.byref(attn(max_pages=100, max_len=128)), C.byref(n)) == 0 and n.value == 0
