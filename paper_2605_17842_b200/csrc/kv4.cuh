@@ -580,7 +580,8 @@ static __global__ void __launch_bounds__(kReadThreads) k_kv4_read(Kv4Rows p, int
 // comes out the same whether it is decoded alone, in a verify block or in a sweep over all layers.
 // Bound: for one row of 160 x 10 heads x 2048 keys (472 MB, 98 us with the join = 4.8 TB/s, 97 us of it here) the copies alone
 // take 84 us and the arithmetic alone 86 us; the codes' masks, shifts and byte moves keep the ALU pipe at 53 % with 12 warps
-// an SM (163 registers, 221 KB of stages).  For prompt chunks the mma.sync rate and the same unpacking: 62 TFLOP/s.
+// an SM (163 registers, 221 KB of stages).  Prompt chunks: the same unpacking once per 16 rows and
+// the latency of two warps a scheduler: 6 ragged ones of <= 200 rows and <= 3000 keys 70 TFLOP/s, 8 x 32 heads x 64 rows x 2048 133.
 // Measured against this arrangement and no better: four blocks an SM at 128 registers (spills, -15 %), two at 255 (-4 %), one
 // block of 12 warps an SM (0), bulk copies into mbarrier stages (0), splits of half (-5 %) and twice the length.
 constexpr int kAttn4Warps = 4, kAttn4Threads = 32 * kAttn4Warps;
