@@ -97,7 +97,7 @@ Kv4Shape kv4_shape(int n_rows, int B, int Hq, int Hkv, int max_len, int tile_row
     sh = 6;
     while (sh < 9 && pairs * (((int64_t)max_len + (1 << sh) - 1) >> sh) > most) ++sh;
   } else if (tile_rows) {
-    sh = 9;
+    sh = pairs < 32 ? 8 : 9;   // (the rows, which are not looked at, bring the rest)
   } else {
     // Many rows a sequence: the longest split that leaves enough units.  128 / 256 / 512 / 1024 keys, us: 10 heads x 40 rows x 4096 keys
     // 20 / 25 / 38 / 47; 36 pairs x 200 rows x 3000 147 / 107 / 104 / 117; 8 x 800 x 3000 134 / 112 / 98 / 114; 64 x 256 x 2048

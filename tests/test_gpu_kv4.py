@@ -467,6 +467,18 @@ def test_attention_many_chunks(S, B, n, hk, G):
     run_attention(S, lens, 1, hk * G, hk, 64, 64, F32)
 
 
+@pytest.mark.parametrize("B,T,hk,G,n", [(1, 9, 2, 1, 900), (3, 40, 4, 4, 1500), (6, 40, 4, 4, 1500), (8, 40, 8, 4, 1100), (13, 40, 8, 4, 1100)])
+def test_attention_every_split_of_prompt_chunks(S, B, T, hk, G, n):
+    """Splits of 64, 128, 256, 512 and 1024 keys, by the number of row tiles."""
+    run_attention(S, [n - 37 * b for b in range(B)], T, hk * G, hk, 64, 64, BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hk,n", [(1, 128), (1, 129), (3, 1030), (40, 2500), (160, 2100)])
+def test_attention_every_split_of_single_tokens(S, hk, n, dtype):
+    run_attention(S, [n, n // 2], 1, hk, hk, 64, 32, dtype)
+
+
 def test_attention_of_thousands_of_sequences(S):
     """More sequences than the kernel's list has entries for, empty ones among them."""
     rng = np.random.default_rng(3)
